@@ -2,7 +2,7 @@
 
 A matrix in 8-bit floats has e4m3 codes, row by row, and for every 128 consecutive entries of a row one scale,
 a power of two (e8m0): the smallest with which the largest entry stays within 448.  Rows of codes are padded with
-zeros to whole blocks; scales lie block by block, [blocks][rows].  Kinds of work:
+zeros to whole blocks; scales lie row by row, padded to four.  Kinds of work:
 
   norm            s = x + residual, root-mean-square norm of s times a weight, into 8-bit floats for the product behind it
   norm_backward   gradients of s and of the weight
@@ -88,7 +88,7 @@ def _padded(n, to):
 
 
 def _codes(x):
-    """fp32 [rows, cols] -> e4m3 codes [rows, cols padded to whole blocks], e8m0 scales [blocks, rows padded to 16]."""
+    """fp32 [rows, cols] -> e4m3 codes [rows, cols padded to whole blocks], e8m0 scales [rows, blocks padded to four]."""
     rows, cols = x.shape
     wide = torch.zeros((rows, _padded(cols, BLOCK)), dtype=torch.float32, device=x.device)
     wide[:, :cols] = x
@@ -98,8 +98,8 @@ def _codes(x):
     e = torch.where(amax > 0, p + 118 + (m > 0.875).int(), torch.zeros_like(p)).clamp(0, 254)
     e = torch.where(torch.isfinite(amax), e, torch.full_like(e, 255))
     codes = torch.ldexp(blocks, (127 - e).unsqueeze(2)).to(torch.float8_e4m3fn).view(rows, -1)
-    scales = torch.zeros((blocks.shape[1], _padded(rows, 16)), dtype=torch.uint8, device=x.device)
-    scales[:, :rows] = e.t().to(torch.uint8)
+    scales = torch.zeros((rows, _padded(blocks.shape[1], 4)), dtype=torch.uint8, device=x.device)
+    scales[:, :blocks.shape[1]] = e.to(torch.uint8)
     return codes, scales.view(torch.float8_e8m0fnu)
 
 
@@ -145,11 +145,11 @@ def prepare(case, seed):
 
 
 # ---- plain forms ------------------------------------------------------------------------------------------------
-def _values(form, rows, cols, to=torch.float32):
+def _values(form, cols, to=torch.float32):
     """The numbers that codes and scales stand for."""
     codes, scales = form
-    s = scales.to(to)[:, :rows].t().unsqueeze(2)
-    return (codes.to(to).view(rows, -1, BLOCK) * s).view(rows, -1)[:, :cols]
+    c = codes.to(to).view(codes.shape[0], -1, BLOCK)
+    return (c * scales.to(to)[:, :c.shape[1]].unsqueeze(2)).view(codes.shape)[:, :cols]
 
 
 def _act(name, g):
@@ -164,7 +164,7 @@ def _act(name, g):
 
 def _eight_bits(x):
     codes, scales = _codes(x)
-    return {"codes": codes[:, :x.shape[1]], "scales": scales[:, :x.shape[0]]}
+    return {"codes": codes[:, :x.shape[1]], "scales": scales[:, :codes.shape[1] // BLOCK]}
 
 
 def _plain(state):
@@ -189,12 +189,12 @@ def _plain(state):
             dx = dx + state["residual"].float()
         return {"dx": dx.to(state["x"].dtype), "dweight": (dy * hat).sum(0)}
     inner = case["inner"]
-    x = _values(state["x"], rows, inner)
-    w = _values(state["w"], cols, inner)
+    x = _values(state["x"], inner)
+    w = _values(state["w"], inner)
     if do == "product":
         return (x @ w.t()).to(TYPES[case["type"]])
     a, da = _act(case["act"], x @ w.t())
-    u = x @ _values(state["u"], cols, inner).t()
+    u = x @ _values(state["u"], inner).t()
     if do == "gated":
         return _eight_bits(a * u)
     dh = state["dh"].float()
@@ -203,7 +203,7 @@ def _plain(state):
 
 # ---- the framework's --------------------------------------------------------------------------------------------
 def _shown(m):
-    return {"codes": m.codes[:, :m.cols], "scales": m.scales[:, :m.rows]}
+    return {"codes": m.codes[:, :m.cols], "scales": m.scales[:, :m.blocks]}
 
 
 def _own(state):
@@ -218,11 +218,11 @@ def _own(state):
     if do == "norm_backward":
         dx, dw = q.qgtc_rms_norm_backward(state["dy"], state["x"], state["weight"], state["rstd"], dsum=state.get("residual"))
         return {"dx": dx, "dweight": dw}
-    x = q.Fp8(*state["x"], cols=case["inner"], rows=case["rows"])
-    w = q.Fp8(*state["w"], cols=case["inner"], rows=case["cols"])
+    x = q.Fp8(*state["x"], cols=case["inner"])
+    w = q.Fp8(*state["w"], cols=case["inner"])
     if do == "product":
         return q.qgtc_fp8_product(x, w, TYPES[case["type"]])
-    u = q.Fp8(*state["u"], cols=case["inner"], rows=case["cols"])
+    u = q.Fp8(*state["u"], cols=case["inner"])
     if do == "gated":
         return _shown(q.qgtc_fp8_gated(x, w, u, case["act"]))
     return q.qgtc_fp8_gated_backward(x, w, u, state["dh"], case["act"])
@@ -263,7 +263,7 @@ def _quotients(y):
         two = torch.where(two * 448 < top, two * 2, torch.where((two / 2 * 448 >= top) & (two > 2.0 ** -127), two / 2, two))
         codes.append(part / two.unsqueeze(1))
         scales.append(two)
-    return {"codes": torch.cat(codes, 1), "scales": torch.stack(scales)}
+    return {"codes": torch.cat(codes, 1), "scales": torch.stack(scales, 1)}
 
 
 def exact(case, seed):
@@ -289,15 +289,15 @@ def exact(case, seed):
         return {"dx": dx, "dweight": torch.einsum("ij,ij,i->j", dy, s, r)}
     inner = case["inner"]
 
-    def whole(form, n):
+    def whole(form):
         codes, scales = form
-        return codes.double()[:, :inner] * scales.double()[:, :n].t().repeat_interleave(BLOCK, 1)[:, :inner]
+        return codes.double()[:, :inner] * scales.double().repeat_interleave(BLOCK, 1)[:, :inner]
 
-    x = whole(state["x"], rows)
-    g = x @ whole(state["w"], cols).t()
+    x = whole(state["x"])
+    g = x @ whole(state["w"]).t()
     if do == "product":
         return g
-    u = x @ whole(state["u"], cols).t()
+    u = x @ whole(state["u"]).t()
     if case["act"] == "silu":
         half = torch.tanh(g / 2)
         a, da = g * (1 + half) / 2, (1 + half) / 2 + g * (1 - half * half) / 4
