@@ -688,6 +688,132 @@ qgtc_status qgtc_fold_batchnorm(const double* gamma, const double* beta, const d
                                 const double* var, double eps, double value_scale, int32_t n,
                                 float* col_scale, float* col_shift);
 
+/* ---------------------------------------------------------------------------
+ * 8-bit floats.  Where a range fixed ahead (Eq. (2)) does not fit - activations whose
+ * rows differ by orders of magnitude, gradients - the scale follows the data: a matrix
+ * has codes of one byte (e4m3: sign, 4 exponent bits, 3 mantissa bits, largest 448, one
+ * NaN per sign) and for each 128 consecutive entries of a row, a block, one scale of one
+ * byte (e8m0: the power of two 2^(byte - 127), 255 NaN):
+ *   value(r, c) = e4m3(codes[r * ld + c]) * 2^(scales[r * ld_scales + c / 128] - 127)
+ * Powers of two, because gfx950's matrix instruction applies them itself.
+ *   ld          bytes between rows: a multiple of 128, at least cols
+ *   ld_scales   a multiple of 4, at least ceil(cols / 128)
+ * codes is 16-byte aligned, scales 4-byte aligned.  Codes between cols and the end of the
+ * row's last block are 0; every entry point that writes the form writes them.  Scales past the last
+ * block are read with the others and enter no result.
+ *
+ * Quantizing a block (everywhere): e is the smallest byte with max|x| <= 448 * 2^(e - 127),
+ * 0 for a block of zeros; code = x * 2^(127 - e), exact but for subnormal results, rounded to
+ * the nearest e4m3, ties to even.  A block with an infinity or a NaN has e = 255 and NaN codes:
+ * all of its values are NaN.
+ *
+ * Other tensors are row-major in one of three types, with a leading dimension in elements
+ * (any that is at least the number of columns) and the alignment of their type.
+ * ------------------------------------------------------------------------- */
+enum { QGTC_F32 = 0, QGTC_F16 = 1, QGTC_BF16 = 2 };
+
+typedef struct qgtc_fp8 {
+  uint8_t* codes;
+  uint8_t* scales;
+  int32_t rows;
+  int32_t cols;
+  int64_t ld;
+  int64_t ld_scales;
+} qgtc_fp8;
+
+/* Fills the scalar fields with the default strides (cols rounded up to 128, blocks rounded up to 4);
+ * the buffers need rows * ld and rows * ld_scales bytes.  QGTC_ERR_SHAPE for negative sizes.  Host-only. */
+qgtc_status qgtc_fp8_describe(qgtc_fp8* d, int32_t rows, int32_t cols);
+
+/* src (rows x cols, QGTC_F32 / F16 / BF16) into 8-bit floats: with columns == 0 dst is rows x cols, else
+ * dst is cols x rows, its blocks lying along src's columns - the operand of a product that contracts over
+ * src's rows (gradients of weights). */
+qgtc_status qgtc_fp8_quantize(const void* src, int32_t type, int32_t rows, int32_t cols, int64_t ld_src,
+                              int32_t columns, const qgtc_fp8* dst, void* stream);
+
+/* Root-mean-square norm with the residual's addition:
+ *   s    = x + residual, rounded to `type` (x itself without a residual)
+ *   rstd = 1 / sqrt(mean of s^2 over the row + eps)
+ *   y    = s * rstd * weight
+ * in fp32, of s as it is rounded.  Any of the outputs may be left out (NULL):
+ *   sum   s, in `type`; may be x or residual themselves (same leading dimension)
+ *   rstd  [rows], for qgtc_rms_norm_backward
+ *   y     in `type`
+ *   out   y as 8-bit floats, quantized from fp32
+ * x, residual (or NULL), sum and y have `type`, weight [cols] has weight_type.  At most 32768 columns
+ * (QGTC_ERR_UNSUPPORTED).  Outputs must not overlap inputs otherwise. */
+typedef struct qgtc_norm {
+  int32_t type, weight_type;
+  int32_t rows, cols;
+  float eps;
+  int32_t reserved;
+  const void* x;
+  int64_t ld_x;
+  const void* residual;
+  int64_t ld_residual;
+  const void* weight;
+  void* sum;
+  int64_t ld_sum;
+  void* y;
+  int64_t ld_y;
+  float* rstd;
+  const qgtc_fp8* out;
+} qgtc_norm;
+qgtc_status qgtc_rms_norm(const qgtc_norm* n, void* stream);
+
+/* Its gradients, from that of y (quantization counts as the identity):
+ *   hat = s * rstd,  g = dy * weight
+ *   dx  = rstd * (g - hat * mean(g * hat)) + dsum        the gradient of x and of the residual
+ *   dweight = sum over the rows of dy * hat              fp32; the same bits for the same inputs
+ * dsum (or NULL) is the gradient that reaches s past the norm.  dy, sum, dsum and dx have `type`; dx may be
+ * dy or dsum themselves.  dweight may be NULL; else
+ * workspace: device, 16-byte aligned, qgtc_rms_norm_backward_workspace_bytes of them. */
+typedef struct qgtc_norm_grad {
+  int32_t type, weight_type;
+  int32_t rows, cols;
+  const void* dy;
+  int64_t ld_dy;
+  const void* sum;
+  int64_t ld_sum;
+  const void* weight;
+  const float* rstd;
+  const void* dsum;
+  int64_t ld_dsum;
+  void* dx;
+  int64_t ld_dx;
+  float* dweight;
+} qgtc_norm_grad;
+size_t qgtc_rms_norm_backward_workspace_bytes(int32_t rows, int32_t cols);
+qgtc_status qgtc_rms_norm_backward(const qgtc_norm_grad* n, void* workspace, size_t workspace_bytes, void* stream);
+
+/* out = X.W' of two matrices in 8-bit floats: X rows x K, W cols x K (a row per output column), sums in fp32,
+ * rounded once to `type`.  The products of a linear layer y = x.w': X = x and W = w give y; X = dy and W = w'
+ * (w quantized with columns = 1) give dx; X = dy and W = x, both with columns = 1, give dw.  K = 0: zeros.
+ * workspace: qgtc_fp8_product_workspace_bytes (0: none is used), 16-byte aligned; NULL, or one that is too small, keeps
+ * the product from being divided along K, which is slower where there are few tiles of output. */
+size_t qgtc_fp8_product_workspace_bytes(int32_t rows, int32_t cols, int32_t inner);
+qgtc_status qgtc_fp8_product(const qgtc_fp8* X, const qgtc_fp8* W, int32_t type, void* out, int64_t ld_out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* The first half of a gated feed-forward block, both projections, the activation and their product in one:
+ *   h = act(X.G') * (X.U')
+ * X: rows x K, G and U: cols x K.  act: QGTC_ACT_SILU, g / (1 + exp(-g)), or QGTC_ACT_GELU, its tanh form
+ * g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))).  out (8-bit floats, quantized from fp32) or h (in `type`) may be NULL.
+ * workspace: qgtc_fp8_gated_workspace_bytes (0: none is used), 16-byte aligned (else QGTC_ERR_WORKSPACE).
+ *
+ * qgtc_fp8_gated_backward: the gradients of the two projections' results, in `type`, from that of h:
+ *   dg = dh * u * act'(g),  du = dh * act(g)
+ * g and u are computed again (they are not kept).  dg and du may be the two halves of one matrix with 2 cols
+ * columns, the form the products behind it want: dX = [dg du].[G; U], [dG; dU] = [dg du]'.X. */
+enum { QGTC_ACT_SILU = 0, QGTC_ACT_GELU = 1 };
+size_t qgtc_fp8_gated_workspace_bytes(int32_t rows, int32_t cols, int32_t inner);
+qgtc_status qgtc_fp8_gated(const qgtc_fp8* X, const qgtc_fp8* G, const qgtc_fp8* U, int32_t act,
+                           const qgtc_fp8* out, int32_t type, void* h, int64_t ld_h,
+                           void* workspace, size_t workspace_bytes, void* stream);
+qgtc_status qgtc_fp8_gated_backward(const qgtc_fp8* X, const qgtc_fp8* G, const qgtc_fp8* U, int32_t act,
+                                    int32_t type, const void* dh, int64_t ld_dh, void* dg, int64_t ld_dg,
+                                    void* du, int64_t ld_du, void* stream);
+
 /* What the library found on the current device, against what its kernels are written
  * for: code objects for gfx950 only, workgroups dealt over 8 XCDs of 32 compute units
  * each (Section 4.3's tile rows are spread so that a subgraph's rows share an XCD's L2),

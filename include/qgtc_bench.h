@@ -28,7 +28,8 @@ enum {
   QGTC_KERNEL_UPDATE = 3,
   QGTC_KERNEL_SUMS = 4,
   QGTC_KERNEL_LAYER = 5, /* fused layer kernel (with its weight re-ordering) */
-  QGTC_KERNEL_KINDS = 6
+  QGTC_KERNEL_NORM = 6,  /* root-mean-square norm and its gradients */
+  QGTC_KERNEL_KINDS = 7
 };
 qgtc_status qgtc_prof_enable(int32_t on);
 qgtc_status qgtc_prof_reset(void);

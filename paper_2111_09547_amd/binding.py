@@ -15,7 +15,7 @@ import torch  # first: the HIP runtime PyTorch ships must be the one libqgtc bin
 LEFT, RIGHT, RIGHT_BYTES, LEFT_BYTES = 0, 1, 2, 3
 SRC_F32, SRC_U8, SRC_I32 = 0, 1, 2
 OUT_I32, OUT_F32, OUT_BITS = 0, 1, 2
-KERNEL_PACK, KERNEL_TILE_MAP, KERNEL_AGGREGATE, KERNEL_UPDATE, KERNEL_SUMS, KERNEL_LAYER = range(6)
+KERNEL_PACK, KERNEL_TILE_MAP, KERNEL_AGGREGATE, KERNEL_UPDATE, KERNEL_SUMS, KERNEL_LAYER, KERNEL_NORM = range(7)
 
 _STATUS = ["ok", "null pointer", "shape mismatch", "bit width out of range",
            "misaligned pointer or leading dimension", "wrong packed layout",
@@ -120,6 +120,26 @@ class _WideStackC(C.Structure):
                 ("n_layers", C.c_int32), ("s", C.c_int32), ("buffer", C.c_void_p * 2), ("buffer_bytes", C.c_size_t)]
 
 
+class _Fp8C(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int32), ("cols", C.c_int32),
+                ("ld", C.c_int64), ("ld_scales", C.c_int64)]
+
+
+class _NormC(C.Structure):
+    _fields_ = [("type", C.c_int32), ("weight_type", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32),
+                ("eps", C.c_float), ("reserved", C.c_int32), ("x", C.c_void_p), ("ld_x", C.c_int64),
+                ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("weight", C.c_void_p),
+                ("sum", C.c_void_p), ("ld_sum", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("rstd", C.c_void_p), ("out", C.POINTER(_Fp8C))]
+
+
+class _NormGradC(C.Structure):
+    _fields_ = [("type", C.c_int32), ("weight_type", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32),
+                ("dy", C.c_void_p), ("ld_dy", C.c_int64), ("sum", C.c_void_p), ("ld_sum", C.c_int64),
+                ("weight", C.c_void_p), ("rstd", C.c_void_p), ("dsum", C.c_void_p), ("ld_dsum", C.c_int64),
+                ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dweight", C.c_void_p)]
+
+
 class _DeviceC(C.Structure):
     _fields_ = [("compute_units", C.c_int32), ("xcds", C.c_int32), ("is_gfx950", C.c_int32),
                 ("xcds_assumed", C.c_int32)]
@@ -192,6 +212,16 @@ def lib():
         "qgtc_fold_batchnorm": (C.c_int, [P(C.c_double), P(C.c_double), P(C.c_double), P(C.c_double),
                                          C.c_double, C.c_double, i32, P(C.c_float), P(C.c_float)]),
         "qgtc_device_info": (C.c_int, [P(_DeviceC)]),
+        "qgtc_fp8_describe": (C.c_int, [P(_Fp8C), i32, i32]),
+        "qgtc_fp8_quantize": (C.c_int, [vp, i32, i32, i32, i64, i32, P(_Fp8C), vp]),
+        "qgtc_rms_norm": (C.c_int, [P(_NormC), vp]),
+        "qgtc_rms_norm_backward_workspace_bytes": (sz, [i32, i32]),
+        "qgtc_rms_norm_backward": (C.c_int, [P(_NormGradC), vp, sz, vp]),
+        "qgtc_fp8_product_workspace_bytes": (sz, [i32, i32, i32]),
+        "qgtc_fp8_product": (C.c_int, [P(_Fp8C), P(_Fp8C), i32, vp, i64, vp, sz, vp]),
+        "qgtc_fp8_gated_workspace_bytes": (sz, [i32, i32, i32]),
+        "qgtc_fp8_gated": (C.c_int, [P(_Fp8C), P(_Fp8C), P(_Fp8C), i32, P(_Fp8C), i32, vp, i64, vp, sz, vp]),
+        "qgtc_fp8_gated_backward": (C.c_int, [P(_Fp8C), P(_Fp8C), P(_Fp8C), i32, i32, vp, i64, vp, i64, vp, i64, vp]),
         "qgtc_probe_popcount": (C.c_int, [i32, i32, i32, C.c_void_p, C.c_void_p]),
         "qgtc_probe_units": (i64, [P(_BitsC), i32, i32, i64, i64, vp, vp, vp]),
         "qgtc_prof_enable": (C.c_int, [i32]),

@@ -1,0 +1,274 @@
+// Products of matrices in 8-bit floats: checks, the choice of a kernel, and the kernel for few rows.
+#include "product.h"
+
+namespace qgtc {
+namespace {
+
+// Few rows: what counts is reading W.  A workgroup has 16 rows of it and 16 MT rows of X; its waves share K in pieces of four
+// blocks, straight from memory to registers, and add up through LDS.
+template <int MODE, int MT, bool WIDE>
+__global__ __launch_bounds__(512) void few_kernel(const ProductParams p) {
+  constexpr int D = MODE == kProduct ? 1 : 2;
+  extern __shared__ v4f box[];                       // [wave][D][MT][lane]
+  const int wave = (int)(threadIdx.x >> 6), waves = (int)(blockDim.x >> 6), lane = (int)(threadIdx.x & 63u);
+  const int r = lane & 15, g = lane >> 4;
+  const int n0 = (int)blockIdx.x * 16, m0 = (int)blockIdx.y * (16 * MT);
+  const uint8_t *wc[D], *ws[D], *xc[MT], *xs[MT];
+#pragma unroll
+  for (int d = 0; d < D; ++d) {
+    const Fp8Operand& w = d ? p.u : p.w;
+    const int64_t n = min(n0 + r, p.cols - 1);
+    wc[d] = w.codes + n * w.ld + 16 * g;
+    ws[d] = w.scales + n * w.ld_scales;
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int64_t m = min(m0 + 16 * t + r, p.rows - 1);
+    xc[t] = p.x.codes + m * p.x.ld + 16 * g;
+    xs[t] = p.x.scales + m * p.x.ld_scales;
+  }
+  v4f acc[D][MT];
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[d][t] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+  for (int b0 = wave * 4; b0 < p.blocks; b0 += waves * 4) {
+    uint32_t sw[D], sx[MT];
+#pragma unroll
+    for (int d = 0; d < D; ++d) sw[d] = *reinterpret_cast<const uint32_t*>(ws[d] + b0);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) sx[t] = *reinterpret_cast<const uint32_t*>(xs[t] + b0);
+    auto one = [&](auto which) {
+      constexpr int B = decltype(which)::value;
+      const int64_t at = (int64_t)(b0 + B) * kBlock;
+      v8i w[D], x[MT];
+#pragma unroll
+      for (int d = 0; d < D; ++d) w[d] = lane_codes(wc[d] + at);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) x[t] = lane_codes(xc[t] + at);
+      if constexpr (WIDE) {
+        WideCodes wide[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) wide[t] = widen<B>(x[t], sx[t]);
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+          const WideCodes v = widen<B>(w[d], sw[d]);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) acc[d][t] = wide_mfma(v, wide[t], acc[d][t]);
+        }
+      } else {
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+#pragma unroll
+          for (int t = 0; t < MT; ++t) acc[d][t] = block_mfma<B>(w[d], x[t], acc[d][t], sw[d], sx[t]);
+      }
+    };
+    if (b0 + 4 <= p.blocks) {
+      one(std::integral_constant<int, 0>());
+      one(std::integral_constant<int, 1>());
+      one(std::integral_constant<int, 2>());
+      one(std::integral_constant<int, 3>());
+    } else {
+      one(std::integral_constant<int, 0>());
+      if (b0 + 1 < p.blocks) one(std::integral_constant<int, 1>());
+      if (b0 + 2 < p.blocks) one(std::integral_constant<int, 2>());
+    }
+  }
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) box[((wave * D + d) * MT + t) * 64 + lane] = acc[d][t];
+  __syncthreads();
+  for (int t = wave; t < MT; t += waves) {
+    v4f sum[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      sum[d] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+      for (int i = 0; i < waves; ++i) {
+        const v4f v = box[((i * D + d) * MT + t) * 64 + lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum[d][k] += v[k];
+      }
+    }
+    const int m = m0 + 16 * t + r, n = n0 + 4 * g, left = p.cols - n;
+    if (m >= p.rows || left <= 0) continue;
+    float a[4], b[4];
+    if constexpr (MODE == kProduct) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[k] = sum[0][k];
+      store4_as(p.type, p.out, (int64_t)m * p.ld_out + n, left, a);
+    } else if constexpr (MODE == kGated) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[k] = gate(p.act, sum[0][k]).value * sum[D - 1][k];
+      if (p.out) store4_as(p.type, p.out, (int64_t)m * p.ld_out + n, left, a);
+      if (p.wide) store4_of<QGTC_F32>(p.wide, (int64_t)m * p.cols + n, left, a);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float dh = k < left ? load_as(p.type, p.dh, (int64_t)m * p.ld_dh + n + k) : 0.0f;
+        const Gate v = gate(p.act, sum[0][k]);
+        a[k] = dh * sum[D - 1][k] * v.slope;
+        b[k] = dh * v.value;
+      }
+      store4_as(p.type, p.out, (int64_t)m * p.ld_out + n, left, a);
+      store4_as(p.type, p.out2, (int64_t)m * p.ld_out2 + n, left, b);
+    }
+  }
+}
+
+template <int MODE, int MT, bool WIDE>
+qgtc_status launch_few(const ProductParams& p, hipStream_t stream) {
+  constexpr int D = MODE == kProduct ? 1 : 2;
+  const int waves = 8;
+  const size_t lds = (size_t)waves * D * MT * 64 * 16;
+  // (a launch has at most 65535 workgroups along the second axis: rows beyond go in launches of their own)
+  const int most = 65535 * 16 * MT;
+  for (int64_t m0 = 0; m0 < p.rows; m0 += most) {
+    ProductParams q = p;
+    q.rows = (int32_t)(p.rows - m0 < most ? p.rows - m0 : most);
+    q.x.codes += m0 * p.x.ld;
+    q.x.scales += m0 * p.x.ld_scales;
+    const int64_t b = float_bytes(p.type);
+    if (q.out) q.out = (char*)p.out + m0 * p.ld_out * b;
+    if (q.out2) q.out2 = (char*)p.out2 + m0 * p.ld_out2 * b;
+    if (q.dh) q.dh = (const char*)p.dh + m0 * p.ld_dh * b;
+    if (q.wide) q.wide += m0 * p.cols;
+    hipLaunchKernelGGL((few_kernel<MODE, MT, WIDE>), dim3((unsigned)cdiv(p.cols, 16), (unsigned)cdiv(q.rows, 16 * MT)), dim3(64u * waves), lds, stream, q);
+    const qgtc_status st = launch_status();
+    if (st != QGTC_OK) return st;
+  }
+  return QGTC_OK;
+}
+
+template <int MODE, bool WIDE>
+qgtc_status launch(const ProductParams& p, hipStream_t stream) {
+  if (p.rows <= 16) return launch_few<MODE, 1, WIDE>(p, stream);
+  if (p.rows <= 32) return launch_few<MODE, 2, WIDE>(p, stream);
+  return launch_few<MODE, 4, WIDE>(p, stream);
+}
+// Results in fp32 have sums that are worth it.
+template <int MODE>
+qgtc_status launch(const ProductParams& p, hipStream_t stream) {
+  return p.out && p.type == QGTC_F32 ? launch<MODE, true>(p, stream) : launch<MODE, false>(p, stream);
+}
+
+Fp8Operand operand(const qgtc_fp8* m) { return {m->codes, m->scales, m->ld, m->ld_scales, m->rows}; }
+
+// X, and the operands that it is multiplied with, of the same sizes.
+qgtc_status check_operands(const qgtc_fp8* X, const qgtc_fp8* W, const qgtc_fp8* U) {
+  qgtc_status st = check_fp8(X);
+  if (st == QGTC_OK) st = check_fp8(W);
+  if (st == QGTC_OK && U) st = check_fp8(U);
+  if (st != QGTC_OK) return st;
+  if (X->cols != W->cols || (U && (U->cols != W->cols || U->rows != W->rows))) return QGTC_ERR_SHAPE;
+  return QGTC_OK;
+}
+
+}  // namespace
+}  // namespace qgtc
+
+extern "C" size_t qgtc_fp8_product_workspace_bytes(int32_t rows, int32_t cols, int32_t inner) {
+  (void)rows; (void)cols; (void)inner;
+  return 0;
+}
+
+extern "C" qgtc_status qgtc_fp8_product(const qgtc_fp8* X, const qgtc_fp8* W, int32_t type, void* out, int64_t ld_out,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace qgtc;
+  (void)workspace_bytes;
+  qgtc_status st = check_operands(X, W, nullptr);
+  if (st != QGTC_OK) return st;
+  if (!float_type(type)) return QGTC_ERR_UNSUPPORTED;
+  if (((uintptr_t)workspace & 15u) != 0) return QGTC_ERR_ALIGN;
+  if (X->rows == 0 || W->rows == 0) return QGTC_OK;
+  if ((st = check_matrix(out, type, X->rows, W->rows, ld_out)) != QGTC_OK) return st;
+  ProductParams p{};
+  p.x = operand(X);
+  p.w = operand(W);
+  p.blocks = fp8_blocks(X->cols);
+  p.rows = X->rows;
+  p.cols = W->rows;
+  p.type = type;
+  p.out = out;
+  p.ld_out = ld_out;
+  const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  ProfScope prof(QGTC_KERNEL_UPDATE, s);
+  return launch<kProduct>(p, s);
+}
+
+extern "C" size_t qgtc_fp8_gated_workspace_bytes(int32_t rows, int32_t cols, int32_t inner) {
+  (void)inner;
+  return rows <= 0 || cols <= 0 ? 0 : (size_t)rows * (size_t)cols * 4;
+}
+
+extern "C" qgtc_status qgtc_fp8_gated(const qgtc_fp8* X, const qgtc_fp8* G, const qgtc_fp8* U, int32_t act,
+                                      const qgtc_fp8* out, int32_t type, void* h, int64_t ld_h,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace qgtc;
+  if (!U) return QGTC_ERR_NULL;
+  qgtc_status st = check_operands(X, G, U);
+  if (st != QGTC_OK) return st;
+  if (act != QGTC_ACT_SILU && act != QGTC_ACT_GELU) return QGTC_ERR_UNSUPPORTED;
+  if (out) {
+    if ((st = check_fp8(out)) != QGTC_OK) return st;
+    if (out->rows != X->rows || out->cols != G->rows) return QGTC_ERR_SHAPE;
+  }
+  if (X->rows == 0 || G->rows == 0) return QGTC_OK;
+  if (!out && !h) return QGTC_ERR_NULL;
+  if (h && (st = check_matrix(h, type, X->rows, G->rows, ld_h)) != QGTC_OK) return st;
+  ProductParams p{};
+  p.x = operand(X);
+  p.w = operand(G);
+  p.u = operand(U);
+  p.blocks = fp8_blocks(X->cols);
+  p.rows = X->rows;
+  p.cols = G->rows;
+  p.type = h ? type : QGTC_F32;
+  p.act = act;
+  p.out = h;
+  p.ld_out = ld_h;
+  if (out) {
+    if (!workspace) return QGTC_ERR_NULL;
+    if (((uintptr_t)workspace & 15u) != 0) return QGTC_ERR_ALIGN;
+    if (workspace_bytes < qgtc_fp8_gated_workspace_bytes(X->rows, G->rows, X->cols)) return QGTC_ERR_WORKSPACE;
+    p.wide = reinterpret_cast<float*>(workspace);
+  }
+  const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  ProfScope prof(QGTC_KERNEL_LAYER, s);
+  st = launch<kGated>(p, s);
+  if (st != QGTC_OK || !out) return st;
+  return quantize_rows(p.wide, QGTC_F32, p.rows, p.cols, p.cols, *out, s);
+}
+
+extern "C" qgtc_status qgtc_fp8_gated_backward(const qgtc_fp8* X, const qgtc_fp8* G, const qgtc_fp8* U, int32_t act,
+                                               int32_t type, const void* dh, int64_t ld_dh, void* dg, int64_t ld_dg,
+                                               void* du, int64_t ld_du, void* stream) {
+  using namespace qgtc;
+  if (!U) return QGTC_ERR_NULL;
+  qgtc_status st = check_operands(X, G, U);
+  if (st != QGTC_OK) return st;
+  if (act != QGTC_ACT_SILU && act != QGTC_ACT_GELU) return QGTC_ERR_UNSUPPORTED;
+  if (!float_type(type)) return QGTC_ERR_UNSUPPORTED;
+  if (X->rows == 0 || G->rows == 0) return QGTC_OK;
+  if ((st = check_matrix(dh, type, X->rows, G->rows, ld_dh)) != QGTC_OK) return st;
+  if ((st = check_matrix(dg, type, X->rows, G->rows, ld_dg)) != QGTC_OK) return st;
+  if ((st = check_matrix(du, type, X->rows, G->rows, ld_du)) != QGTC_OK) return st;
+  ProductParams p{};
+  p.x = operand(X);
+  p.w = operand(G);
+  p.u = operand(U);
+  p.blocks = fp8_blocks(X->cols);
+  p.rows = X->rows;
+  p.cols = G->rows;
+  p.type = type;
+  p.act = act;
+  p.out = dg;
+  p.ld_out = ld_dg;
+  p.out2 = du;
+  p.ld_out2 = ld_du;
+  p.dh = dh;
+  p.ld_dh = ld_dh;
+  const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  ProfScope prof(QGTC_KERNEL_LAYER, s);
+  return launch<kGatedGrad>(p, s);
+}
