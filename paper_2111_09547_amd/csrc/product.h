@@ -5,6 +5,10 @@
 
 namespace qgtc {
 
+struct ProductParams;
+// Tiles of 256 x 256 (product_tile.hip), for results of 16 and 8 bits.
+template <int MODE> qgtc_status launch_tiles(const ProductParams& p, hipStream_t stream);
+
 enum { kProduct = 0, kGated = 1, kGatedGrad = 2 };  // what is made of the sums
 
 struct Fp8Operand {
@@ -93,6 +97,7 @@ __device__ __forceinline__ float exp_minus(float z) {
 struct Gate {
   float value, slope;
 };
+template <bool PRECISE>
 __device__ __forceinline__ Gate gate(int act, float g) {
   float z = g, dz = 1.0f;
   if (act == QGTC_ACT_GELU) {
@@ -100,8 +105,14 @@ __device__ __forceinline__ Gate gate(int act, float g) {
     z = k * fmaf(0.044715f * g2, g, g);
     dz = k * fmaf(0.134145f, g2, 1.0f);
   }
-  const float e = exp_minus(z), s = __builtin_amdgcn_rcpf(1.0f + e);
-  return {g * s, s * fmaf(g * dz, e * s, 1.0f)};     // 1 - s = e s
+  if constexpr (PRECISE) {
+    const float e = exp_minus(z), s = __builtin_amdgcn_rcpf(1.0f + e);
+    return {g * s, s * fmaf(g * dz, e * s, 1.0f)};     // 1 - s = e s
+  } else {
+    // For results of 16 and 8 bits: off by |z| 2^-24 of the sigmoid, which is below 2^-16 where it is not below 2^-360 itself.
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+    return {g * s, s * fmaf(g * dz, 1.0f - s, 1.0f)};
+  }
 }
 
 // Four entries of a row from column c on.

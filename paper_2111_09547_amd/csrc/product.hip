@@ -1,6 +1,8 @@
 // Products of matrices in 8-bit floats: checks, the choice of a kernel, and the kernel for few rows.
 #include "product.h"
 
+#include <initializer_list>
+
 namespace qgtc {
 namespace {
 
@@ -99,14 +101,14 @@ __global__ __launch_bounds__(512) void few_kernel(const ProductParams p) {
       store4_as(p.type, p.out, (int64_t)m * p.ld_out + n, left, a);
     } else if constexpr (MODE == kGated) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) a[k] = gate(p.act, sum[0][k]).value * sum[D - 1][k];
+      for (int k = 0; k < 4; ++k) a[k] = gate<true>(p.act, sum[0][k]).value * sum[D - 1][k];
       if (p.out) store4_as(p.type, p.out, (int64_t)m * p.ld_out + n, left, a);
       if (p.wide) store4_of<QGTC_F32>(p.wide, (int64_t)m * p.cols + n, left, a);
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float dh = k < left ? load_as(p.type, p.dh, (int64_t)m * p.ld_dh + n + k) : 0.0f;
-        const Gate v = gate(p.act, sum[0][k]);
+        const Gate v = gate<true>(p.act, sum[0][k]);
         a[k] = dh * sum[D - 1][k] * v.slope;
         b[k] = dh * v.value;
       }
@@ -146,12 +148,15 @@ qgtc_status launch(const ProductParams& p, hipStream_t stream) {
   if (p.rows <= 32) return launch_few<MODE, 2, WIDE>(p, stream);
   return launch_few<MODE, 4, WIDE>(p, stream);
 }
-// Results in fp32 have sums that are worth it.
+// Whether tiles are taken (results in fp32 have sums that are worth it, and none of those).
+bool many_rows(int rows) { return rows > 128; }
 template <int MODE>
 qgtc_status launch(const ProductParams& p, hipStream_t stream) {
-  return p.out && p.type == QGTC_F32 ? launch<MODE, true>(p, stream) : launch<MODE, false>(p, stream);
+  if (p.out && p.type == QGTC_F32) return launch<MODE, true>(p, stream);
+  return many_rows(p.rows) && p.blocks > 0 ? launch_tiles<MODE>(p, stream) : launch<MODE, false>(p, stream);
 }
 
+constexpr int64_t kMostLd = 1 << 24;
 Fp8Operand operand(const qgtc_fp8* m) { return {m->codes, m->scales, m->ld, m->ld_scales, m->rows}; }
 
 // X, and the operands that it is multiplied with, of the same sizes.
@@ -160,6 +165,9 @@ qgtc_status check_operands(const qgtc_fp8* X, const qgtc_fp8* W, const qgtc_fp8*
   if (st == QGTC_OK) st = check_fp8(W);
   if (st == QGTC_OK && U) st = check_fp8(U);
   if (st != QGTC_OK) return st;
+  // (a tile's rows are addressed with 32 bits)
+  for (const qgtc_fp8* m : {X, W, U})
+    if (m && (m->ld > kMostLd || m->ld_scales > kMostLd || (int64_t)fp8_blocks(m->cols) * kBlock >= kMostLd)) return QGTC_ERR_UNSUPPORTED;
   if (X->cols != W->cols || (U && (U->cols != W->cols || U->rows != W->rows))) return QGTC_ERR_SHAPE;
   return QGTC_OK;
 }
@@ -197,8 +205,7 @@ extern "C" qgtc_status qgtc_fp8_product(const qgtc_fp8* X, const qgtc_fp8* W, in
 }
 
 extern "C" size_t qgtc_fp8_gated_workspace_bytes(int32_t rows, int32_t cols, int32_t inner) {
-  (void)inner;
-  return rows <= 0 || cols <= 0 ? 0 : (size_t)rows * (size_t)cols * 4;
+  return rows <= 0 || cols <= 0 || (qgtc::many_rows(rows) && inner > 0) ? 0 : (size_t)rows * (size_t)cols * 4;
 }
 
 extern "C" qgtc_status qgtc_fp8_gated(const qgtc_fp8* X, const qgtc_fp8* G, const qgtc_fp8* U, int32_t act,
@@ -227,17 +234,26 @@ extern "C" qgtc_status qgtc_fp8_gated(const qgtc_fp8* X, const qgtc_fp8* G, cons
   p.act = act;
   p.out = h;
   p.ld_out = ld_h;
-  if (out) {
-    if (!workspace) return QGTC_ERR_NULL;
-    if (((uintptr_t)workspace & 15u) != 0) return QGTC_ERR_ALIGN;
-    if (workspace_bytes < qgtc_fp8_gated_workspace_bytes(X->rows, G->rows, X->cols)) return QGTC_ERR_WORKSPACE;
-    p.wide = reinterpret_cast<float*>(workspace);
+  const bool from_h = out && h && type == QGTC_F32;       // h is what is quantized
+  if (out && !from_h) {
+    const size_t need = qgtc_fp8_gated_workspace_bytes(X->rows, G->rows, X->cols);
+    if (need) {
+      if (!workspace) return QGTC_ERR_NULL;
+      if (((uintptr_t)workspace & 15u) != 0) return QGTC_ERR_ALIGN;
+      if (workspace_bytes < need) return QGTC_ERR_WORKSPACE;
+      p.wide = reinterpret_cast<float*>(workspace);
+    } else {
+      p.codes = out->codes;
+      p.scales = out->scales;
+      p.ld_codes = out->ld;
+      p.ld_scales = out->ld_scales;
+    }
   }
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   ProfScope prof(QGTC_KERNEL_LAYER, s);
   st = launch<kGated>(p, s);
-  if (st != QGTC_OK || !out) return st;
-  return quantize_rows(p.wide, QGTC_F32, p.rows, p.cols, p.cols, *out, s);
+  if (st != QGTC_OK || !out || p.codes) return st;
+  return from_h ? quantize_rows(h, QGTC_F32, p.rows, p.cols, ld_h, *out, s) : quantize_rows(p.wide, QGTC_F32, p.rows, p.cols, p.cols, *out, s);
 }
 
 extern "C" qgtc_status qgtc_fp8_gated_backward(const qgtc_fp8* X, const qgtc_fp8* G, const qgtc_fp8* U, int32_t act,

@@ -130,6 +130,9 @@ def test_product_refuses(b):
     assert call(type=3) == UNSUPPORTED
     assert call(out=0x30002) == ALIGN and call(type=2, out=0x30001) == ALIGN and call(ws=0x40004) == ALIGN
     assert call(x=form(b, 8, 300, ld=448)) == ALIGN and call(w=form(b, 20, 300, codes=0x10004)) == ALIGN
+    for more in ({"ld": (1 << 24) + 128}, {"ld_scales": (1 << 24) + 4}):
+        assert call(x=form(b, 8, 300, **more)) == UNSUPPORTED and call(w=form(b, 20, 300, **more)) == UNSUPPORTED
+    assert call(x=form(b, 8, 1 << 24), w=form(b, 20, 1 << 24)) == UNSUPPORTED
     assert call(x=form(b, 0, 300), out=None) == OK and call(w=form(b, 0, 300), out=None) == OK
 
 
@@ -147,8 +150,8 @@ def test_gated_refuses(b):
     assert call(out=form(b, 8, 21)) == SHAPE and call(out=form(b, 7, 20)) == SHAPE and call(out=form(b, 8, 20, scales=None)) == NULL
     need = size(8, 20, 300)
     if need:
-        assert call(out=form(b, 8, 20), ws=None) == NULL and call(out=form(b, 8, 20), ws=0x40008) == ALIGN
-        assert call(out=form(b, 8, 20), nbytes=need - 1) == WORKSPACE
+        assert call(out=form(b, 8, 20), ws=None, type=2) == NULL and call(out=form(b, 8, 20), ws=0x40008, type=2) == ALIGN
+        assert call(out=form(b, 8, 20), nbytes=need - 1, type=2) == WORKSPACE and call(out=form(b, 8, 20), h=None, ws=None) == NULL
     assert size(0, 20, 300) == 0 and size(8, 0, 300) == 0
     assert call(x=form(b, 0, 300), h=None, out=form(b, 0, 20)) == OK
 
