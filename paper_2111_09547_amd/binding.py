@@ -130,7 +130,7 @@ class _NormC(C.Structure):
                 ("eps", C.c_float), ("reserved", C.c_int32), ("x", C.c_void_p), ("ld_x", C.c_int64),
                 ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("weight", C.c_void_p),
                 ("sum", C.c_void_p), ("ld_sum", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64),
-                ("rstd", C.c_void_p), ("out", C.POINTER(_Fp8C))]
+                ("rstd", C.c_void_p), ("out", C.c_void_p)]    # out: of an _Fp8C
 
 
 class _NormGradC(C.Structure):

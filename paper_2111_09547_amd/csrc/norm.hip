@@ -171,18 +171,22 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_grad_kernel(const GradP
   for (int i = 0; i < V; ++i) store8_of<QGTC_F32>(p.partial + (int64_t)blockIdx.x * p.cols, c0 + i * kPiece, p.cols, dw[i]);
 }
 
-// 32 columns of the groups' shares: a thread adds up every 32nd share of one column after the other's, and the threads' sums
-// are added in order.
+// Eight columns of the groups' shares: a thread adds up the shares of every 32nd group, four loads ahead of the sum, and the threads'
+// sums are added in order.
+constexpr int kSumColumns = 8;
 __global__ __launch_bounds__(256) void norm_grad_sum_kernel(const float* partial, float* dweight, int cols, int groups) {
-  __shared__ float box[8][33];
-  const int c = (int)blockIdx.x * 32 + (int)(threadIdx.x & 31u), k = (int)(threadIdx.x >> 5);
+  __shared__ float box[32][kSumColumns + 1];
+  const int c = (int)blockIdx.x * kSumColumns + (int)(threadIdx.x & 7u), k = (int)(threadIdx.x >> 3);
   float s = 0.0f;
-  if (c < cols)
-    for (int g = k; g < groups; g += 8) s += partial[(int64_t)g * cols + c];
-  box[k][threadIdx.x & 31u] = s;
+  if (c < cols) {
+#pragma unroll 4
+    for (int g = k; g < groups; g += 32) s += partial[(int64_t)g * cols + c];
+  }
+  box[k][threadIdx.x & 7u] = s;
   __syncthreads();
   if (k == 0 && c < cols) {
-    for (int i = 1; i < 8; ++i) s += box[i][threadIdx.x & 31u];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) s += box[i][threadIdx.x & 7u];
     dweight[c] = s;
   }
 }
@@ -324,6 +328,6 @@ extern "C" qgtc_status qgtc_rms_norm_backward(const qgtc_norm_grad* n, void* wor
     st = n->type == QGTC_F32 ? launch_grad<QGTC_F32>(p, s) : n->type == QGTC_F16 ? launch_grad<QGTC_F16>(p, s) : launch_grad<QGTC_BF16>(p, s);
     if (st != QGTC_OK || !n->dweight) return st;
   }
-  hipLaunchKernelGGL(norm_grad_sum_kernel, dim3((unsigned)cdiv(n->cols, 32)), dim3(256), 0, s, p.partial, n->dweight, n->cols, p.groups);
+  hipLaunchKernelGGL(norm_grad_sum_kernel, dim3((unsigned)cdiv(n->cols, kSumColumns)), dim3(256), 0, s, p.partial, n->dweight, n->cols, p.groups);
   return launch_status();
 }

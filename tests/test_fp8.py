@@ -78,7 +78,7 @@ def test_norm_refuses(b):
     def call(out=None, **more):
         n = b._NormC(0, 0, 8, 300, 1e-6, 0, 0x10000, 300, None, 0, 0x20000, 0x30000, 300, 0x40000, 300, 0x50000)
         if out is not None:
-            n.out = C.pointer(out)
+            n.out = C.addressof(out)
         for k, v in more.items():
             setattr(n, k, v)
         return f(C.byref(n), None)
