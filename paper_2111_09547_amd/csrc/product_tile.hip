@@ -17,7 +17,9 @@
 //
 // A row of a buffer is 128 bytes; its 16-byte piece c lies at c ^ (row % 8), so that 16 lanes reading a piece each of 16 rows meet
 // every bank once.  W's rows are put into the buffer in another order: register i of lane group g of the t-th 16 of 64 belongs
-// to row 16 g + 4 i + t of them, so that a lane ends up with 16 results that lie side by side.
+// to row 32 (t / 2) + 8 g + 4 (t % 2) + i of them, so that a lane ends up with twice eight results that lie side by side, and four
+// lanes with 32, or, where results are bytes, to row 16 g + 4 t + i, and a lane has 16 side by side: 64 bytes of a row for a store
+// either way (the other order for bytes: gated 4096 x 4096 x 8192 233 instead of 226 us).
 #include "product.h"
 
 namespace qgtc {
@@ -70,6 +72,7 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
 
   // ---- which tiles: an XCD's are neighbours, in groups that are 8 tiles of rows high; its workgroups take them in turn ----
   constexpr int TN = MODE == kProduct ? kTile : kTile / 2;           // columns of the result
+  constexpr bool kBytes = MODE == kGated;
   const uint32_t first = (blockIdx.x & 7u) * tp.per_xcd, turn = gridDim.x >> 3;
   const uint32_t behind = min(first + tp.per_xcd, tp.tiles_m * tp.tiles_n);
   uint32_t id = first + (blockIdx.x >> 3);
@@ -100,21 +103,21 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
     rw[1] = both ? buffer_of(p.u.codes + (int64_t)n0 * p.u.ld, most_w * (uint32_t)p.u.ld + row_bytes) : rw[0];
     rsw = buffer_of(w_scales + (int64_t)n0 * w_ld_scales, most_w * (uint32_t)w_ld_scales + row_words);
   };
-  // rows 128 pair + 64 h + 32 part + 8 j + lane / 8 of X's buffer, which are X's; of W's buffer, which are, of 64, W's 4 (i % 16) + i / 16
+  // rows 128 pair + 64 h + 32 part + 8 j + lane / 8 of X's buffer, which are X's; and of W's
   const uint32_t ldx = (uint32_t)p.x.ld, ldw[2] = {(uint32_t)p.w.ld, both ? (uint32_t)p.u.ld : (uint32_t)p.w.ld};
   const uint32_t xoff = (uint32_t)(128 * pair + 32 * part + (lane >> 3)) * ldx + piece;
   uint32_t woff[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) woff[h] = (uint32_t)((both ? 64 : 128) * pair + 2 * part + 4 * (lane >> 3)) * ldw[h] + piece;
+  for (int h = 0; h < 2; ++h) woff[h] = (uint32_t)((both ? 64 : 128) * pair + (kBytes ? 8 : 32) * part + (kBytes ? 16 : 8) * (lane >> 5) + (lane >> 3 & 3)) * ldw[h] + piece;
   const uint32_t sxoff = (uint32_t)(64 * wave + lane) * (uint32_t)p.x.ld_scales;
-  const uint32_t swoff = (uint32_t)((both ? 64 * pair : 64 * wave) + 4 * r + g) * (uint32_t)w_ld_scales;
+  const uint32_t swoff = (uint32_t)((both ? 64 * pair : 64 * wave) + (kBytes ? 4 * g + 16 * (r >> 2) : 32 * (g >> 1) + 8 * (r >> 2) + 4 * (g & 1)) + (r & 3)) * (uint32_t)w_ld_scales;
   const uint32_t to_x = lds0 + (uint32_t)(128 * pair + 32 * part) * kBlock, to_w = to_x + kOperand;
   uint32_t load_id = id;
   int load_step = 0, load_slot = 0;
   auto load_one = [&](uint32_t buffer, int h, int j) {   // an eighth of a wave's loads of a block's halves h
     const uint32_t at = buffer + (uint32_t)(64 * h) * kBlock + (uint32_t)(j & 3) * 1024u, from = (uint32_t)load_step * kBlock;
     if (j < 4) load16_lds(rx, xoff, from + (uint32_t)(64 * h + 8 * j) * ldx, to_x + at);
-    else load16_lds(rw[h], woff[h], from + (uint32_t)((both ? 0 : 64 * h) + 32 * (j & 1) + (j >> 1 & 1)) * ldw[h], to_w + at);
+    else load16_lds(rw[h], woff[h], from + (uint32_t)((both ? 0 : 64 * h) + (kBytes ? 32 : 16) * (j & 1) + 4 * (j >> 1 & 1)) * ldw[h], to_w + at);
   };
   auto load_scales = [&] {                               // in front of every fourth block
     if ((load_step & 3) != 0) return;
@@ -161,11 +164,15 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
     }
   };
 
-  // ---- what is made of the sums: lane (r, g) has row 16 t + r of each half of x and 16 columns from 16 g on of each half of w ----
+  // ---- what is made of the sums: lane (r, g) has row 16 u + r of each half of x, and of each half of w the columns 32 k + 8 g + j (bytes:
+  // 8 k + 16 g + j), k = 0, 1 and j = 0..7, in register j % 4 of the sums 2 k + j / 4 ----
+  auto store8 = [&](void* to, int64_t ld, int m, int n, const float (&v)[8]) {
+    if (p.type == QGTC_F16) store8_of<QGTC_F16>((uint16_t*)to + (int64_t)m * ld, n, p.cols, v);
+    else store8_of<QGTC_BF16>((uint16_t*)to + (int64_t)m * ld, n, p.cols, v);
+  };
   auto finish = [&](uint32_t tile) {
     int m0, bn;
     place(tile, m0, bn);
-    const int n0 = bn * TN;
     auto row_of = [&](int hx, int u) { return m0 + wm * 128 + hx * 64 + u * 16 + r; };
     if constexpr (MODE == kProduct) {
 #pragma unroll
@@ -173,46 +180,38 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int m = row_of(hx, u);
-          if (m >= p.rows) continue;
+          if (m < p.rows) {
 #pragma unroll
-          for (int hw = 0; hw < 2; ++hw) {
-            const int n = n0 + wn * 128 + hw * 64 + 16 * g, left = p.cols - n;
-            float v[2][8];
+            for (int q = 0; q < 4; ++q) {
+              float v[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i >> 3][i & 7] = acc[hw][hx][i & 3][u][i >> 2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              if (p.type == QGTC_F16) store8_of<QGTC_F16>((uint16_t*)p.out + (int64_t)m * p.ld_out + n, 8 * k, left, v[k]);
-              else store8_of<QGTC_BF16>((uint16_t*)p.out + (int64_t)m * p.ld_out + n, 8 * k, left, v[k]);
+              for (int j = 0; j < 8; ++j) v[j] = acc[q >> 1][hx][2 * (q & 1) + (j >> 2)][u][j & 3];
+              store8(p.out, p.ld_out, m, bn * TN + wn * 128 + 32 * q + 8 * g, v);
             }
           }
         }
     } else if constexpr (MODE == kGated) {
-      const int n = n0 + wn * 64 + 16 * g, left = p.cols - n;
+      const int n0 = bn * TN + wn * 64 + 16 * g;
+      const bool whole = bn * TN + TN <= p.cols;
       uint32_t* const tops = reinterpret_cast<uint32_t*>(lds + kTops);
 #pragma unroll
       for (int hx = 0; hx < 2; ++hx)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
+          const int m = row_of(hx, u);
           uint32_t top = 0u;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float h = gate<false>(p.act, acc[0][hx][i & 3][u][i >> 2]).value * acc[1][hx][i & 3][u][i >> 2];
-            h = i < left ? h : 0.0f;
-            acc[0][hx][i & 3][u][i >> 2] = h;
-            top = max(top, abs_bits(h));
-          }
-          if (p.out) {
-            const int m = row_of(hx, u);
-            float v[2][8];
+          for (int k = 0; k < 2; ++k) {
+            float v[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i >> 3][i & 7] = acc[0][hx][i & 3][u][i >> 2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              if (m >= p.rows) continue;
-              if (p.type == QGTC_F16) store8_of<QGTC_F16>((uint16_t*)p.out + (int64_t)m * p.ld_out + n, 8 * k, left, v[k]);
-              else store8_of<QGTC_BF16>((uint16_t*)p.out + (int64_t)m * p.ld_out + n, 8 * k, left, v[k]);
+            for (int j = 0; j < 8; ++j) {
+              const int t = 2 * k + (j >> 2);
+              const float h = gate<false>(p.act, acc[0][hx][t][u][j & 3]).value * acc[1][hx][t][u][j & 3];
+              v[j] = whole || n0 + 8 * k + j < p.cols ? h : 0.0f;
+              acc[0][hx][t][u][j & 3] = v[j];
             }
+            top = max(top, abs_max(v));
+            if (p.out && m < p.rows) store8(p.out, p.ld_out, m, n0 + 8 * k, v);
           }
           top = max(top, (uint32_t)__shfl_xor((int)top, 16));
           top = max(top, (uint32_t)__shfl_xor((int)top, 32));
@@ -225,43 +224,44 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int m = row_of(hx, u), lr = wm * 128 + hx * 64 + u * 16 + r;
-          if (m >= p.rows) continue;
-          const uint32_t e = scale_byte(max(tops[lr], tops[kTile + lr]));
-          u32x4 c;
+          if (m < p.rows) {
+            const uint32_t e = scale_byte(max(tops[lr], tops[kTile + lr]));
+            u32x4 c;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            c[k] = encode4(acc[0][hx][0][u][k], acc[0][hx][1][u][k], acc[0][hx][2][u][k], acc[0][hx][3][u][k], e);
-            if (e == 255u && left < 4 * k + 4) c[k] &= left <= 4 * k ? 0u : 0xffffffffu >> (8 * (4 * k + 4 - left));   // (zeros past the end)
+            for (int t = 0; t < 4; ++t) {
+              const v4f& v = acc[0][hx][t][u];
+              c[t] = encode4(v[0], v[1], v[2], v[3], e);
+              const int left = p.cols - (n0 + 4 * t);
+              if (e == 255u && left < 4) c[t] &= left <= 0 ? 0u : 0xffffffffu >> (8 * (4 - left));   // (zeros past the end)
+            }
+            *reinterpret_cast<u32x4*>(p.codes + (int64_t)m * p.ld_codes + n0) = c;
+            if (g == 0 && wn == 0) p.scales[(int64_t)m * p.ld_scales + bn] = (uint8_t)e;
           }
-          *reinterpret_cast<u32x4*>(p.codes + (int64_t)m * p.ld_codes + n) = c;
-          if (g == 0 && wn == 0) p.scales[(int64_t)m * p.ld_scales + bn] = (uint8_t)e;
         }
+      // (the next tile's largest values are written a barrier of its products later)
     } else {
-      const int n = n0 + wn * 64 + 16 * g, left = p.cols - n;
+      const int n0 = bn * TN + wn * 64 + 8 * g;
 #pragma unroll
       for (int hx = 0; hx < 2; ++hx)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int m = row_of(hx, u);
-          if (m >= p.rows || left <= 0) continue;
+          if (m < p.rows) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float dh[8], dg[8], du[8];
-            if (p.type == QGTC_F16) load8_of<QGTC_F16>((const uint16_t*)p.dh + (int64_t)m * p.ld_dh + n, 8 * k, left, dh);
-            else load8_of<QGTC_BF16>((const uint16_t*)p.dh + (int64_t)m * p.ld_dh + n, 8 * k, left, dh);
+            for (int k = 0; k < 2; ++k) {
+              const int n = n0 + 32 * k;
+              float dh[8], dg[8], du[8];
+              if (p.type == QGTC_F16) load8_of<QGTC_F16>((const uint16_t*)p.dh + (int64_t)m * p.ld_dh, n, p.cols, dh);
+              else load8_of<QGTC_BF16>((const uint16_t*)p.dh + (int64_t)m * p.ld_dh, n, p.cols, dh);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int i = 8 * k + j;
-              const Gate v = gate<false>(p.act, acc[0][hx][i & 3][u][i >> 2]);
-              dg[j] = dh[j] * acc[1][hx][i & 3][u][i >> 2] * v.slope;
-              du[j] = dh[j] * v.value;
-            }
-            if (p.type == QGTC_F16) {
-              store8_of<QGTC_F16>((uint16_t*)p.out + (int64_t)m * p.ld_out + n, 8 * k, left, dg);
-              store8_of<QGTC_F16>((uint16_t*)p.out2 + (int64_t)m * p.ld_out2 + n, 8 * k, left, du);
-            } else {
-              store8_of<QGTC_BF16>((uint16_t*)p.out + (int64_t)m * p.ld_out + n, 8 * k, left, dg);
-              store8_of<QGTC_BF16>((uint16_t*)p.out2 + (int64_t)m * p.ld_out2 + n, 8 * k, left, du);
+              for (int j = 0; j < 8; ++j) {
+                const int t = 2 * k + (j >> 2);
+                const Gate v = gate<false>(p.act, acc[0][hx][t][u][j & 3]);
+                dg[j] = dh[j] * acc[1][hx][t][u][j & 3] * v.slope;
+                du[j] = dh[j] * v.value;
+              }
+              store8(p.out, p.ld_out, m, n, dg);
+              store8(p.out2, p.ld_out2, m, n, du);
             }
           }
         }
