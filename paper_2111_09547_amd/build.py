@@ -16,7 +16,7 @@ OBJ_DIR = os.path.join(PKG, "_build")
 SOURCES = ["api.hip", "plan.hip", "pack.hip", "host_pack.hip", "tilemap.hip", "lists.hip", "gather.hip",
            "gather_m0.hip", "gather_m1.hip", "gather_m2.hip", "gather_m3.hip", "gather_wide.hip", "first_product.hip", "aggregate.hip", "agg_dense.hip", "layer.hip",
            "layer_n0.hip", "layer_n1.hip", "layer_n4.hip", "layer_n16.hip", "stack.hip", "update.hip", "update_mfma.hip", "probe.hip",
-           "quantize.hip", "norm.hip", "product.hip", "product_tile.hip"]
+           "quantize.hip", "norm.hip", "product.hip", "product_tile.hip", "product_mid.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",

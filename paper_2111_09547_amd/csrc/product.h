@@ -8,6 +8,8 @@ namespace qgtc {
 struct ProductParams;
 // Tiles of 256 x 256 (product_tile.hip), for results of 16 and 8 bits.
 template <int MODE> qgtc_status launch_tiles(const ProductParams& p, hipStream_t stream);
+// Tiles of 128 x 128 (product_mid.hip); wide: with fp32's sums.
+template <int MODE> qgtc_status launch_mid(const ProductParams& p, bool wide, hipStream_t stream);
 
 enum { kProduct = 0, kGated = 1, kGatedGrad = 2 };  // what is made of the sums
 
@@ -136,6 +138,19 @@ __device__ __forceinline__ float load_as(int type, const void* base, int64_t at)
   if (type == QGTC_F32) return Float<QGTC_F32>::load((const float*)base + at);
   if (type == QGTC_F16) return Float<QGTC_F16>::load((const uint16_t*)base + at);
   return Float<QGTC_BF16>::load((const uint16_t*)base + at);
+}
+// Eight entries of row m from column n on.  WIDE: fp32, else one of the types of 16 bits.
+template <bool WIDE>
+__device__ __forceinline__ void store8_as(int type, void* base, int64_t ld, int m, int n, int cols, const float (&v)[8]) {
+  if constexpr (WIDE) store8_of<QGTC_F32>((float*)base + (int64_t)m * ld, n, cols, v);
+  else if (type == QGTC_F16) store8_of<QGTC_F16>((uint16_t*)base + (int64_t)m * ld, n, cols, v);
+  else store8_of<QGTC_BF16>((uint16_t*)base + (int64_t)m * ld, n, cols, v);
+}
+template <bool WIDE>
+__device__ __forceinline__ void load8_as(int type, const void* base, int64_t ld, int m, int n, int cols, float (&v)[8]) {
+  if constexpr (WIDE) load8_of<QGTC_F32>((const float*)base + (int64_t)m * ld, n, cols, v);
+  else if (type == QGTC_F16) load8_of<QGTC_F16>((const uint16_t*)base + (int64_t)m * ld, n, cols, v);
+  else load8_of<QGTC_BF16>((const uint16_t*)base + (int64_t)m * ld, n, cols, v);
 }
 
 #endif  // __HIPCC__

@@ -143,17 +143,46 @@ qgtc_status launch_few(const ProductParams& p, hipStream_t stream) {
 }
 
 template <int MODE, bool WIDE>
-qgtc_status launch(const ProductParams& p, hipStream_t stream) {
+qgtc_status launch_few(const ProductParams& p, hipStream_t stream) {
   if (p.rows <= 16) return launch_few<MODE, 1, WIDE>(p, stream);
   if (p.rows <= 32) return launch_few<MODE, 2, WIDE>(p, stream);
   return launch_few<MODE, 4, WIDE>(p, stream);
 }
-// Whether tiles are taken (results in fp32 have sums that are worth it, and none of those).
-bool many_rows(int rows) { return rows > 128; }
+
+// Which kernel: the one that takes least by what each was measured to take, in us (bf16 results, M x N x K; few, mid, tiles):
+//   product  32 x 4096 x 4096   9.1  17.8  43.5     gated  32 x 4096 x 4096  14.7  21.3  49.3
+//           128 x 4096 x 4096  23.5  18.0  46.0           128 x 4096 x 4096  33.0  23.0  52.0
+//           128 x 1024 x 1024   5.3   7.3  17.3          1024 x 1024 x 1024  24.2  13.9  23.4
+//          1024 x 4096 x 4096   161  21.9  47.8          1024 x 4096 x 4096   216  47.5  54.6
+//          4096 x 4096 x 4096         84.1  60.8          512 x 8192 x 2048   118  32.1  35.3
+//          8192 x 2048 x 8192          160   109         4096 x 4096 x 4096   846   174   116
+// few: its workgroups' reads, 16 rows of W and of X each, at 8 TB/s.  mid and tiles: rounds of tiles, a block of K at a time (a block
+// takes longer where all compute units are busy and the clock falls), and what they start and end with.  Gated blocks that are not
+// made by tiles pass their results through memory and another launch.
+enum Path { kFew, kMid, kTiles };
+Path path_of(int mode, int rows, int cols, int blocks, bool wide) {
+  if (blocks == 0) return kFew;
+  const bool two = mode != kProduct;
+  const int cus = device_compute_units(), per_few = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  const double again = mode == kGated && !wide ? 3.5 + (double)rows * cols * 8 / 6e6 : 0.0;
+  const double few = 2.5 + (double)cdiv(cols, 16) * cdiv(rows, per_few) * ((two ? 32 : 16) + per_few) * blocks * kBlock / 8.2e6 + again;
+  const int64_t mids = (int64_t)cdiv(rows, 128) * cdiv(cols, two ? 64 : 128);
+  const double mid = 4.0 + (double)cdiv(mids, cus) * blocks * (wide ? 1.05 : mids <= cus / 2 ? 0.45 : 0.6) + again;
+  const Path less = few <= mid ? kFew : kMid;
+  if (wide) return less;
+  const int64_t tiles = (int64_t)cdiv(rows, 256) * cdiv(cols, two ? 128 : 256);
+  const double tile = (two ? 14.0 : 8.0) + (double)cdiv(tiles, cus) * blocks * (tiles <= cus / 2 ? 1.2 : 1.6);
+  return tile < (less == kFew ? few : mid) ? kTiles : less;
+}
+
 template <int MODE>
 qgtc_status launch(const ProductParams& p, hipStream_t stream) {
-  if (p.out && p.type == QGTC_F32) return launch<MODE, true>(p, stream);
-  return many_rows(p.rows) && p.blocks > 0 ? launch_tiles<MODE>(p, stream) : launch<MODE, false>(p, stream);
+  const bool wide = p.out && p.type == QGTC_F32;   // results in fp32 have sums that are worth it
+  switch (path_of(MODE, p.rows, p.cols, p.blocks, wide)) {
+    case kTiles: return launch_tiles<MODE>(p, stream);
+    case kMid: return launch_mid<MODE>(p, wide, stream);
+    default: return wide ? launch_few<MODE, true>(p, stream) : launch_few<MODE, false>(p, stream);
+  }
 }
 
 constexpr int64_t kMostLd = 1 << 24;
@@ -205,7 +234,8 @@ extern "C" qgtc_status qgtc_fp8_product(const qgtc_fp8* X, const qgtc_fp8* W, in
 }
 
 extern "C" size_t qgtc_fp8_gated_workspace_bytes(int32_t rows, int32_t cols, int32_t inner) {
-  return rows <= 0 || cols <= 0 || (qgtc::many_rows(rows) && inner > 0) ? 0 : (size_t)rows * (size_t)cols * 4;
+  if (rows <= 0 || cols <= 0 || inner < 0) return 0;
+  return qgtc::path_of(qgtc::kGated, rows, cols, qgtc::fp8_blocks(inner), false) == qgtc::kTiles ? 0 : (size_t)rows * (size_t)cols * 4;
 }
 
 extern "C" qgtc_status qgtc_fp8_gated(const qgtc_fp8* X, const qgtc_fp8* G, const qgtc_fp8* U, int32_t act,

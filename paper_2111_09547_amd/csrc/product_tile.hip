@@ -20,7 +20,7 @@
 // to row 32 (t / 2) + 8 g + 4 (t % 2) + i of them, so that a lane ends up with twice eight results that lie side by side, and four
 // lanes with 32, or, where results are bytes, to row 16 g + 4 t + i, and a lane has 16 side by side: 64 bytes of a row for a store
 // either way (the other order for bytes: gated 4096 x 4096 x 8192 233 instead of 226 us).
-#include "product.h"
+#include "product_lds.h"
 
 namespace qgtc {
 namespace {
@@ -38,29 +38,6 @@ struct TileParams {
   uint32_t tiles_m, tiles_n, per_group;            // per_group: tiles of 8 rows of tiles, which are dealt together
   uint32_t per_xcd;
 };
-
-// Wave-wide loads straight to LDS address `to` (+ 16 or 4 bytes per lane); assembly because the compiler would make every later
-// read of LDS wait for them.  What lies behind the buffer's end is not read (LDS gets zeros).  The scalar offset is held to the
-// buffer's size: the unit compares the lane's offset with size - scalar offset, which must not wrap.
-__device__ __forceinline__ void load16_lds(const v4i& rsrc, uint32_t voff, uint32_t soff, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
-               :: "v"(voff), "s"(rsrc), "s"(min(soff, (uint32_t)rsrc[2])), "s"(to) : "m0");
-}
-__device__ __forceinline__ void load4_lds(const v4i& rsrc, uint32_t voff, uint32_t soff, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dword %0, %1, %2 offen lds"
-               :: "v"(voff), "s"(rsrc), "s"(min(soff, (uint32_t)rsrc[2])), "s"(to) : "m0");
-}
-__device__ __forceinline__ uint32_t scalar(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
-__device__ __forceinline__ v4i buffer_of(const void* base, uint32_t bytes) {
-  const uint64_t b = (uint64_t)base;
-  return (v4i){(int)scalar((uint32_t)b), (int)scalar((uint32_t)(b >> 32)), (int)scalar(bytes), 0x00020000};
-}
-
-// What this wave has asked of LDS has come, and of memory all but the last LATER loads; then every wave's.
-template <int LATER>
-__device__ __forceinline__ void meet() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LATER) : "memory");
-}
 
 template <int MODE>
 __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
