@@ -151,8 +151,7 @@ __device__ __forceinline__ uint32_t max_of_16_lanes(uint32_t v) {   // rotations
 }
 
 // Codes of a lane's eight entries from column c on, of a block shared by 16 consecutive lanes, and the block's scale.
-__device__ __forceinline__ void write_block8(uint8_t* codes, uint8_t* scales, int c, int cols, const float (&v)[8]) {
-  const uint32_t e = scale_byte(max_of_16_lanes(abs_max(v)));
+__device__ __forceinline__ void write_block8(uint8_t* codes, uint8_t* scales, int c, int cols, const float (&v)[8], uint32_t e) {
   if ((c & ~(kBlock - 1)) >= cols) return;
   u32x2 w = {encode4(v[0], v[1], v[2], v[3], e), encode4(v[4], v[5], v[6], v[7], e)};
   if (e == 255u && c + 8 > cols) {                 // (zeros past the end, whatever the block)
@@ -162,6 +161,10 @@ __device__ __forceinline__ void write_block8(uint8_t* codes, uint8_t* scales, in
   }
   *reinterpret_cast<u32x2*>(codes + c) = w;
   if ((c & (kBlock - 1)) == 0) scales[c / kBlock] = (uint8_t)e;
+}
+
+__device__ __forceinline__ void write_block8(uint8_t* codes, uint8_t* scales, int c, int cols, const float (&v)[8]) {
+  write_block8(codes, scales, c, cols, v, scale_byte(max_of_16_lanes(abs_max(v))));
 }
 
 #endif  // __HIPCC__

@@ -149,6 +149,25 @@ qgtc_status launch_few(const ProductParams& p, hipStream_t stream) {
   return launch_few<MODE, 4, WIDE>(p, stream);
 }
 
+// h from memory into 8-bit floats: 16 lanes have a block, a wave 512 columns of a row.
+__global__ __launch_bounds__(256) void gated_rows_kernel(const ProductParams p, uint32_t groups) {
+  const uint32_t unit = blockIdx.x * 4u + (threadIdx.x >> 6);
+  const int m = (int)(unit / groups), c = (int)(unit % groups) * 512 + (int)(threadIdx.x & 63u) * 8;
+  if (m >= p.rows) return;
+  float v[8];
+  load8_of<QGTC_F32>(p.wide + (int64_t)m * p.cols, c, p.cols, v);
+  uint32_t top = max_of_16_lanes(abs_max(v));
+  const bool near = near_border(top);
+  if (__ballot(near)) {
+    uint32_t want = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) want |= near && abs_bits(v[i]) >= border_from(top) ? 1u << i : 0u;
+    const uint32_t block = max_of_16_lanes(exact_top(p, m, c, want));
+    if (near) top = block;
+  }
+  write_block8(p.codes + (int64_t)m * p.ld_codes, p.scales + (int64_t)m * p.ld_scales, c, p.cols, v, scale_byte(top));
+}
+
 // Which kernel: the one that takes least by what each was measured to take, in us (bf16 results, M x N x K; few, mid, tiles):
 //   product  32 x 4096 x 4096   9.1  17.8  43.5     gated  32 x 4096 x 4096  14.7  21.3  49.3
 //           128 x 4096 x 4096  23.5  18.0  46.0           128 x 4096 x 4096  33.0  23.0  52.0
@@ -272,18 +291,21 @@ extern "C" qgtc_status qgtc_fp8_gated(const qgtc_fp8* X, const qgtc_fp8* G, cons
       if (((uintptr_t)workspace & 15u) != 0) return QGTC_ERR_ALIGN;
       if (workspace_bytes < need) return QGTC_ERR_WORKSPACE;
       p.wide = reinterpret_cast<float*>(workspace);
-    } else {
-      p.codes = out->codes;
-      p.scales = out->scales;
-      p.ld_codes = out->ld;
-      p.ld_scales = out->ld_scales;
     }
+    p.codes = out->codes;
+    p.scales = out->scales;
+    p.ld_codes = out->ld;
+    p.ld_scales = out->ld_scales;
   }
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   ProfScope prof(QGTC_KERNEL_LAYER, s);
   st = launch<kGated>(p, s);
-  if (st != QGTC_OK || !out || p.codes) return st;
-  return from_h ? quantize_rows(h, QGTC_F32, p.rows, p.cols, ld_h, *out, s) : quantize_rows(p.wide, QGTC_F32, p.rows, p.cols, p.cols, *out, s);
+  if (st != QGTC_OK || !out) return st;
+  if (from_h) return quantize_rows(h, QGTC_F32, p.rows, p.cols, ld_h, *out, s);
+  if (!p.wide) return QGTC_OK;
+  const uint32_t groups = (uint32_t)cdiv(p.cols, 512);
+  hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)(((int64_t)groups * p.rows + 3) / 4)), dim3(256), 0, s, p, groups);
+  return launch_status();
 }
 
 extern "C" qgtc_status qgtc_fp8_gated_backward(const qgtc_fp8* X, const qgtc_fp8* G, const qgtc_fp8* U, int32_t act,

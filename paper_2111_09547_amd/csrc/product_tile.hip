@@ -30,8 +30,8 @@ constexpr int kOperand = kTile * kBlock;           // bytes of an operand's bloc
 constexpr int kBuffer = 2 * kOperand;              // X, then W
 constexpr int kScales = 2 * kBuffer;               // words of four blocks' scales: [4 slots][X, W][256]
 constexpr int kSlot = 2 * kTile * 4;
-constexpr int kTops = kScales + 4 * kSlot;         // largest values of rows: [2][256]
-constexpr int kTileLds = kTops + 2 * kTile * 4;
+constexpr int kTops = kScales + 4 * kSlot;         // largest values of rows: [2][256], and where they have been computed again
+constexpr int kTileLds = kTops + 2 * 2 * kTile * 4;
 
 struct TileParams {
   ProductParams p;
@@ -196,13 +196,39 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
         }
       if (!p.codes) return;
       __syncthreads();
+      uint32_t* const again = tops + 2 * kTile;
+      uint32_t near = 0u;                                // 16 rows in which the exact largest value is wanted
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int lr = wm * 128 + i * 16 + r;
+        const uint32_t mine = tops[wn * kTile + lr];
+        near |= __ballot(near_border(max(mine, tops[(wn ^ 1) * kTile + lr]))) ? 1u << i : 0u;
+        if (g == 0) again[wn * kTile + lr] = mine;
+      }
+#pragma unroll 1
+      for (; near; near &= near - 1u) {                  // (once, not for every 16 rows: the loop of products has to stay in the cache)
+        const int i = __ffs(near) - 1, lr = wm * 128 + i * 16 + r, m = m0 + lr;
+        const uint32_t top = max(tops[lr], tops[kTile + lr]), from = m < p.rows && near_border(top) ? border_from(top) : 0xffffffffu;
+        uint32_t want = 0u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (j != i) continue;
+#pragma unroll
+          for (int k = 0; k < 16; ++k) want |= abs_bits(acc[0][j >> 2][k >> 2][j & 3][k & 3]) >= from ? 1u << k : 0u;
+        }
+        uint32_t exact = exact_top(p, m, n0, want);
+        exact = max(exact, (uint32_t)__shfl_xor((int)exact, 16));
+        exact = max(exact, (uint32_t)__shfl_xor((int)exact, 32));
+        if (g == 0 && from != 0xffffffffu) again[wn * kTile + lr] = exact;
+      }
+      __syncthreads();
 #pragma unroll
       for (int hx = 0; hx < 2; ++hx)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int m = row_of(hx, u), lr = wm * 128 + hx * 64 + u * 16 + r;
           if (m < p.rows) {
-            const uint32_t e = scale_byte(max(tops[lr], tops[kTile + lr]));
+            const uint32_t e = scale_byte(max(again[lr], again[kTile + lr]));
             u32x4 c;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {

@@ -326,6 +326,26 @@ def test_gated_and_its_gradients(act, rows, cols, inner):
             U.close(got[:, at:at + cols], want, np.abs(d) * tf * 1.01 + 2.0 ** -23 * np.abs(want) + U.rounded_tol(want, dtype), (at, dtype))
 
 
+@pytest.mark.parametrize("rows,cols,inner", [(8, 8192, 512), (512, 8192, 520), (4096, 8192, 512)])
+def test_gated_scales_are_those_of_fp32_sums(rows, cols, inner):
+    """Every block's scale, but where the largest entry lies within 2^-18 of a border between two (sums of 512 products in fp32 are off
+    by 512 * 2^-24 of the sum of their sizes at the very worst, by some 2^-22 of the largest entries in fact; the 8-bit instruction by
+    2^-16 and more, which would miss several of 262144 blocks)."""
+    ops = [q.qgtc_fp8_quantize(t.cuda()) for t in (U.activations(rows, inner, 1), U.weights(cols, inner, 2), U.weights(cols, inner, 3))]
+
+    def whole(m):
+        return m.codes.double()[:, :inner] * m.scales.double().repeat_interleave(128, 1)[:, :inner]
+    x, wg, wu = (whole(m) for m in ops)
+    g, u = x @ wg.t(), x @ wu.t()
+    top = (g * torch.sigmoid(g) * u).abs().view(rows, -1, 128).amax(2)
+    m, p = torch.frexp(top)
+    e = p + 118 + (m > 0.875).int()
+    got = q.qgtc_fp8_gated(*ops).scales.view(torch.uint8)[:, :cols // 128].int()
+    unsure = ((m - 0.875).abs() < 0.875 * 2.0 ** -18)
+    assert ((got == e) | unsure).all(), int(((got != e) & ~unsure).sum())
+    print(int((got != e).sum()), "of", got.numel(), "beside the border")
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 def test_gate_far_out(act):
     """Gates of a size where the exponential leaves fp32's range: the activation is the identity or nothing."""
