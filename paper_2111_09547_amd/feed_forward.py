@@ -1,0 +1,71 @@
+"""A pre-norm gated feed-forward block on 8-bit floats, for the dense layers around a quantized network:
+
+    s = x + residual        h = act(n.gate') * (n.up'),  n = norm(s)        y = h.down'
+
+Only the calls are put together here; the arithmetic is in the kernels.  Between them activations are in 8-bit floats: a forward
+pass is three calls, four launches at most.  For training the block keeps what its backward pass wants."""
+from __future__ import annotations
+
+import torch
+
+from . import fp8 as F
+
+
+class GatedFeedForward:
+    """norm_weight [D], gate and up [H, D], down [D, H]: float32, float16 or bfloat16 on one device, quantized once by pack().
+    training: forward() keeps its intermediate results until backward()."""
+
+    def __init__(self, norm_weight: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor, eps: float = 1e-6,
+                 act: str = "silu", training: bool = False):
+        if gate.shape != up.shape or down.shape != (gate.shape[1], gate.shape[0]) or norm_weight.shape != (gate.shape[1],):
+            raise ValueError("gate and up: H x D, down: D x H, norm_weight: D")
+        self.norm_weight, self.gate, self.up, self.down = norm_weight, gate, up, down
+        self.eps, self.act, self.training = eps, act, training
+        self._kept = None
+        self.pack()
+
+    def pack(self):
+        """Weights into 8-bit floats; to be called again when any of them has changed.  For training also along the other axis,
+        as the backward pass contracts over it."""
+        self.gate_q, self.up_q, self.down_q = (F.qgtc_fp8_quantize(w) for w in (self.gate, self.up, self.down))
+        if self.training:
+            self.down_t = F.qgtc_fp8_quantize(self.down, columns=True)
+            self.gate_up_t = F.qgtc_fp8_quantize(torch.cat([self.gate, self.up]), columns=True)
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
+        """(y, s) of x [T, D]: the block's result, which the next norm adds to s."""
+        n = F.qgtc_rms_norm(x, self.norm_weight, self.eps, residual=residual, y=self.training, rstd=self.training)
+        h = torch.empty((x.shape[0], self.gate.shape[0]), dtype=x.dtype, device=x.device) if self.training else None
+        hq = F.qgtc_fp8_gated(n.fp8, self.gate_q, self.up_q, self.act, h=h)
+        if self.training:
+            self._kept = (n, h)
+        return F.qgtc_fp8_product(hq, self.down_q, x.dtype), n.sum
+
+    def backward(self, dy: torch.Tensor, dsum: torch.Tensor | None = None) -> dict:
+        """Gradients of the last forward() from that of y and, unless None, that of s: of x and of the residual ("x", one for both)
+        and of the weights ("norm_weight", "gate", "up", "down": float32).  Quantization counts as the identity."""
+        if self._kept is None:
+            raise RuntimeError("backward() follows a forward() of a block that is training")
+        (n, h), self._kept = self._kept, None
+        hidden, f32 = self.gate.shape[0], torch.float32
+        down = F.qgtc_fp8_product(F.qgtc_fp8_quantize(dy, columns=True), F.qgtc_fp8_quantize(h, columns=True), f32)
+        dh = F.qgtc_fp8_product(F.qgtc_fp8_quantize(dy), self.down_t, dy.dtype)
+        d = F.qgtc_fp8_gated_backward(n.fp8, self.gate_q, self.up_q, dh, self.act)
+        gate_up = F.qgtc_fp8_product(F.qgtc_fp8_quantize(d, columns=True), F.qgtc_fp8_quantize(n.y, columns=True), f32)
+        dn = F.qgtc_fp8_product(F.qgtc_fp8_quantize(d), self.gate_up_t, dy.dtype)
+        dx, dw = F.qgtc_rms_norm_backward(dn, n.sum, self.norm_weight, n.rstd, dsum=dsum)
+        return {"x": dx, "norm_weight": dw, "gate": gate_up[:hidden], "up": gate_up[hidden:], "down": down}
+
+    def capture(self, x: torch.Tensor, residual: torch.Tensor | None = None):
+        """(graph, y, s): one forward pass on these tensors as a HIP graph; a replay reads what x and residual hold then."""
+        if self.training:
+            raise RuntimeError("a block that is training is not recorded")
+        stream = torch.cuda.Stream(x.device)
+        stream.wait_stream(torch.cuda.current_stream(x.device))
+        with torch.cuda.stream(stream):                  # what is done once per kernel is done outside the recording
+            self.forward(x, residual)
+        torch.cuda.current_stream(x.device).wait_stream(stream)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y, s = self.forward(x, residual)
+        return graph, y, s

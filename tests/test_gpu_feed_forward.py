@@ -1,0 +1,177 @@
+"""Norm, gate and product together, as a feed-forward block runs them: every step against its formula in 64 bits on what the
+step before has left, eagerly, recorded, on another stream, and backwards."""
+import numpy as np
+import pytest
+import torch
+
+import fp8_util as U
+
+pytestmark = pytest.mark.gpu
+
+q = pytest.importorskip("paper_2111_09547_amd")
+from paper_2111_09547_amd.feed_forward import GatedFeedForward  # noqa: E402
+
+
+def block(d, h, dtype, act, training=False):
+    t = lambda v: v.to(dtype).cuda()                      # noqa: E731
+    w = 1 + 0.2 * torch.randn(d, generator=torch.Generator().manual_seed(9))
+    return GatedFeedForward(t(w), t(U.weights(h, d, 1)), t(U.weights(h, d, 2)), t(U.weights(d, h, 3)), act=act, training=training)
+
+
+def values(m):
+    return U.fp8_values(m)
+
+
+def product_close(got, x, w):
+    want = values(x) @ values(w).T
+    tol = U.product_tol(values(x), values(w), got.dtype == torch.float32)
+    U.close(got, want, tol * 1.01 + U.rounded_tol(want, got.dtype))
+
+
+@pytest.mark.parametrize("dtype", U.TYPES)
+@pytest.mark.parametrize("rows,d,h", [(1, 256, 512), (33, 200, 300), (300, 384, 640)])
+def test_forward_is_its_steps(dtype, rows, d, h):
+    b = block(d, h, dtype, "silu")
+    x, res = (U.activations(rows, d, k).to(dtype).cuda() for k in (4, 5))
+    y, s = b.forward(x, res)
+    n = q.qgtc_rms_norm(x, b.norm_weight, b.eps, residual=res)
+    hq = q.qgtc_fp8_gated(n.fp8, b.gate_q, b.up_q)
+    assert torch.equal(s, n.sum) and torch.equal(y, q.qgtc_fp8_product(hq, b.down_q, dtype))
+    g = U.gated(values(n.fp8), values(b.gate_q), values(b.up_q), "silu")
+    U.check_codes(hq, g[0], g[1] * 1.01 + 2.0 ** -149)
+    product_close(y, hq, b.down_q)
+    # and the whole of it near the block without 8 bits: four roundings to e4m3 of 2^-5 of an entry on average and less
+    f = [t.double().cpu() for t in (s, b.norm_weight, b.gate, b.up, b.down)]
+    m = f[0] / torch.sqrt(f[0].square().mean(1, keepdim=True) + b.eps) * f[1]
+    want = (torch.nn.functional.silu(m @ f[2].T) * (m @ f[3].T)) @ f[4].T
+    assert float((y.double().cpu() - want).norm() / want.norm()) < 4 * 2.0 ** -4
+
+
+@pytest.mark.parametrize("dtype,act", [(torch.bfloat16, "silu"), (torch.float32, "gelu"), (torch.float16, "gelu")])
+@pytest.mark.parametrize("rows,d,h", [(1, 130, 256), (150, 256, 300), (513, 384, 512)])
+def test_gradients(dtype, act, rows, d, h):
+    b = block(d, h, dtype, act, training=True)
+    x, res, ds = (U.activations(rows, d, k).to(dtype).cuda() for k in (4, 5, 6))
+    dy = (0.1 * torch.randn((rows, d), generator=torch.Generator().manual_seed(7))).to(dtype).cuda()
+    y, s = b.forward(x, res)
+    (n, kept), f32 = b._kept, torch.float32
+    grads = b.backward(dy, ds)
+    with pytest.raises(RuntimeError):
+        b.backward(dy, ds)
+    # each step from what the kernels in front of it have left
+    quant = q.qgtc_fp8_quantize
+    product_close(grads["down"], quant(dy, columns=True), quant(kept, columns=True))
+    dh = q.qgtc_fp8_product(quant(dy), b.down_t, dtype)
+    product_close(dh, quant(dy), b.down_t)
+    h64, th, fg, tfg, a, ta = U.gated(values(n.fp8), values(b.gate_q), values(b.up_q), act, dtype == f32)
+    d2 = q.qgtc_fp8_gated_backward(n.fp8, b.gate_q, b.up_q, dh, act)
+    for at, f, tf in ((0, fg, tfg), (h, a, ta)):
+        want = U.f64(dh) * f
+        U.close(d2[:, at:at + h], want, np.abs(U.f64(dh)) * tf * 1.01 + 2.0 ** -23 * np.abs(want) + U.rounded_tol(want, dtype))
+    whole = torch.cat([grads["gate"], grads["up"]])
+    product_close(whole, quant(d2, columns=True), quant(n.y, columns=True))
+    dn = q.qgtc_fp8_product(quant(d2), b.gate_up_t, dtype)
+    product_close(dn, quant(d2), b.gate_up_t)
+    dx, dw = q.qgtc_rms_norm_backward(dn, s, b.norm_weight, n.rstd, dsum=ds)
+    assert torch.equal(dx, grads["x"]) and torch.equal(dw, grads["norm_weight"])
+    # and the whole of them near the gradients without 8 bits (a chain of at most ten roundings to e4m3, each 2^-5 on average)
+    p = [t.double().cpu().requires_grad_() for t in (s, b.norm_weight, b.gate, b.up, b.down)]
+    m = p[0] / torch.sqrt(p[0].square().mean(1, keepdim=True) + b.eps) * p[1]
+    fn = torch.nn.functional.silu if act == "silu" else lambda v: torch.nn.functional.gelu(v, approximate="tanh")
+    ((fn(m @ p[2].T) * (m @ p[3].T)) @ p[4].T).backward(dy.double().cpu())
+    for name, v in zip(("x", "norm_weight", "gate", "up", "down"), p):
+        got, want = grads[name].double().cpu(), v.grad + (ds.double().cpu() if name == "x" else 0)
+        assert float((got - want).norm() / want.norm()) < 10 * 2.0 ** -5, name
+
+
+@pytest.mark.parametrize("rows", [1, 40, 600])
+def test_recorded_passes(rows):
+    """Two recorded blocks of one size, replayed in turn with eager work between: every replay is the eager pass on what its inputs
+    hold then."""
+    b, c = block(384, 640, torch.bfloat16, "silu"), block(384, 640, torch.bfloat16, "gelu")
+    make = lambda k: U.activations(rows, 384, k).bfloat16().cuda()      # noqa: E731
+    x1, r1, x2 = make(1), make(2), make(3)
+    g1, y1, s1 = b.capture(x1, r1)
+    g2, y2, s2 = c.capture(x2)
+    assert s2 is x2
+    for k in range(4):
+        x1.copy_(make(10 + k))
+        r1.copy_(make(20 + k))
+        x2.copy_(make(30 + k))
+        g1.replay()
+        g2.replay()
+        torch.cuda.synchronize()
+        want1, want2 = b.forward(x1.clone(), r1.clone()), c.forward(x2.clone())
+        assert torch.equal(y1, want1[0]) and torch.equal(s1, want1[1]) and torch.equal(y2, want2[0])
+
+
+def test_recorded_gradients():
+    """Each operator's gradients in one graph, replayed several times."""
+    rows, d, h = 200, 256, 384
+    b = block(d, h, torch.bfloat16, "silu", training=True)
+    n = q.qgtc_rms_norm(U.activations(rows, d, 1).bfloat16().cuda(), b.norm_weight, rstd=True, y=True)
+    dh, dn = (torch.randn((rows, k), device="cuda").bfloat16() for k in (h, d))
+
+    def step():
+        d2 = q.qgtc_fp8_gated_backward(n.fp8, b.gate_q, b.up_q, dh)
+        w = q.qgtc_fp8_product(q.qgtc_fp8_quantize(d2, columns=True), q.qgtc_fp8_quantize(n.y, columns=True), torch.float32)
+        return (d2, w) + tuple(q.qgtc_rms_norm_backward(dn, n.sum, b.norm_weight, n.rstd))
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    for k in range(4):
+        dh.copy_(torch.randn((rows, h), device="cuda"))
+        dn.copy_(torch.randn((rows, d), device="cuda"))
+        g.replay()
+        torch.cuda.synchronize()
+        for a, w in zip(got, step()):
+            assert torch.equal(a, w)
+
+
+def test_another_stream():
+    """Work goes to the stream that is current, behind what is in front of it there."""
+    b = block(512, 1024, torch.bfloat16, "silu")
+    x = U.activations(300, 512, 1).bfloat16().cuda()
+    want, _ = b.forward(x)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        late = torch.zeros_like(x)
+        for _ in range(20):
+            late = late + 1
+        late.copy_(x)
+        y, _ = b.forward(late)
+        z = y.clone()
+    side.synchronize()
+    assert torch.equal(z, want)
+
+
+def test_the_same_bits_every_time():
+    b = block(640, 900, torch.bfloat16, "silu", training=True)
+    x, dy = (U.activations(700, 640, k).bfloat16().cuda() for k in (1, 2))
+    runs = []
+    for _ in range(3):
+        y, _ = b.forward(x)
+        runs.append((y, b.backward(dy)))
+    for y, g in runs[1:]:
+        assert torch.equal(y, runs[0][0]) and all(torch.equal(g[k], runs[0][1][k]) for k in g)
+
+
+def test_refuses():
+    b = block(256, 300, torch.float32, "silu")
+    with pytest.raises(ValueError):
+        b.forward(torch.zeros((4, 255), device="cuda"))
+    with pytest.raises(TypeError):
+        b.forward(torch.zeros((4, 256), device="cuda"), torch.zeros((4, 256), device="cuda", dtype=torch.bfloat16))
+    with pytest.raises(RuntimeError):
+        b.backward(torch.zeros((4, 256), device="cuda"))
+    with pytest.raises(ValueError):
+        GatedFeedForward(b.norm_weight, b.gate, b.up, b.gate)
+    with pytest.raises(q.QgtcError):
+        q.qgtc_fp8_product(q.alloc_fp8(4, 256, "cuda"), q.alloc_fp8(4, 300, "cuda"))
+    with pytest.raises(KeyError):
+        q.qgtc_fp8_gated(q.alloc_fp8(4, 256, "cuda"), b.gate_q, b.up_q, "tanh")
