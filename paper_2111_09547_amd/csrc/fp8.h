@@ -128,14 +128,17 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
   const int e = (int)(amax >> 23) - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
   return (uint32_t)max(e, 0);
 }
-// 2^(127 - e) for the scales of finite blocks (at most 247).
-__device__ __forceinline__ float scale_inverse(uint32_t e) { return __uint_as_float((254u - min(e, 253u)) << 23); }
-// Four codes.  The instruction rounds to the nearest even; nothing is above 448 here.
+// 2^(e - 127).
+__device__ __forceinline__ float scale_value(uint32_t e) { return __uint_as_float(e ? e << 23 : 0x00400000u); }
+// Four codes of values over scale_value(e).  The instruction divides by the power of two and rounds to the nearest even; nothing is
+// above 448 here.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, uint32_t e) {
-  const float inv = scale_inverse(e);
-  uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
-  w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, (int)w, true);
-  return e == 255u ? 0x7f7f7f7fu : w;
+  const float two = scale_value(e);
+  s16x2 w = {0, 0};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, two, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, two, true);
+  return e == 255u ? 0x7f7f7f7fu : __builtin_bit_cast(uint32_t, w);
 }
 
 // The maximum over 16 consecutive lanes, which hold a block of 8 entries each.

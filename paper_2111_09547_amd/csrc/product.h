@@ -62,7 +62,7 @@ struct WideCodes {
 template <int B>
 __device__ __forceinline__ WideCodes widen(const v8i& codes, uint32_t scales) {
   const uint32_t e = scales >> (8 * B) & 255u;
-  const float two = __uint_as_float(e ? e << 23 : 0x00400000u);   // (255: the codes are NaN by themselves)
+  const float two = scale_value(e);                // (255: the codes are NaN by themselves)
   WideCodes w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -119,7 +119,7 @@ __device__ __forceinline__ Gate gate(int act, float g) {
 
 // The scale of a block of h is that of sums in fp32, although sums of the 8-bit instruction are cut: where the block's largest entry lies
 // within 2^-11 of a border between two scales (the cuts move it by some 2^-17, and now and then by 2^-12), the entries that near
-// are computed again, a wave an entry, in two blocks of a thousand.  4096 x 4096 x 8192: 253 us, and 232 without, when 6 of 262144 scales
+// are computed again, a wave an entry, in two blocks of a thousand.  4096 x 4096 x 8192: 233 us, and some 215 without, when 6 of 262144 scales
 // are the other of the two.
 constexpr uint32_t kNear = 1u << 12;               // in units of 2^-23
 __device__ __forceinline__ bool near_border(uint32_t top) {

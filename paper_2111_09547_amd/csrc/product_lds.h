@@ -29,5 +29,9 @@ __device__ __forceinline__ void meet() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LATER) : "memory");
 }
 
+__device__ __forceinline__ void meet_lds() {       // LDS alone: loads and stores stay on their way
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 }  // namespace qgtc
 #endif  // __HIPCC__

@@ -39,7 +39,7 @@ struct TileParams {
   uint32_t per_xcd;
 };
 
-template <int MODE>
+template <int MODE, int TYPE>
 __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
   const ProductParams& p = tp.p;
   extern __shared__ __align__(128) uint8_t lds[];
@@ -143,14 +143,22 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
 
   // ---- what is made of the sums: lane (r, g) has row 16 u + r of each half of x, and of each half of w the columns 32 k + 8 g + j (bytes:
   // 8 k + 16 g + j), k = 0, 1 and j = 0..7, in register j % 4 of the sums 2 k + j / 4 ----
-  auto store8 = [&](void* to, int64_t ld, int m, int n, const float (&v)[8]) {
-    if (p.type == QGTC_F16) store8_of<QGTC_F16>((uint16_t*)to + (int64_t)m * ld, n, p.cols, v);
-    else store8_of<QGTC_BF16>((uint16_t*)to + (int64_t)m * ld, n, p.cols, v);
-  };
+  typedef typename Float<TYPE>::type T;
   auto finish = [&](uint32_t tile) {
+    // (Anew for every tile: what the compiler makes of these once for all tiles it keeps in scratch memory, and each load of it from
+    // there waits for everything that is on its way: gated 4096 x 4096 x 8192 253 us, so 233.)
+    int own = lane;
+    asm volatile("" : "+v"(own));
+    const int r = own & 15, g = own >> 4;
     int m0, bn;
     place(tile, m0, bn);
+    const bool whole = bn * TN + TN <= p.cols;           // (a branch for all lanes: the other way is long)
     auto row_of = [&](int hx, int u) { return m0 + wm * 128 + hx * 64 + u * 16 + r; };
+    auto store8 = [&](void* base, int64_t ld, int m, int n, const float (&v)[8]) {
+      T* const to = (T*)base + (int64_t)m * ld;
+      if (whole) Float<TYPE>::store8(to + n, v);
+      else store8_of<TYPE>(to, n, p.cols, v);
+    };
     if constexpr (MODE == kProduct) {
 #pragma unroll
       for (int hx = 0; hx < 2; ++hx)
@@ -169,33 +177,37 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
         }
     } else if constexpr (MODE == kGated) {
       const int n0 = bn * TN + wn * 64 + 16 * g;
-      const bool whole = bn * TN + TN <= p.cols;
       uint32_t* const tops = reinterpret_cast<uint32_t*>(lds + kTops);
+      float h[8][16];                                    // (in the registers that operands of the products leave)
 #pragma unroll
       for (int hx = 0; hx < 2; ++hx)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int m = row_of(hx, u);
           uint32_t top = 0u;
+          // (columns past the end are products with the zeros that were loaded there)
+          auto gates = [&](int act) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float v[8];
+            for (int j = 0; j < 16; ++j) h[hx * 4 + u][j] = gate<false>(act, acc[0][hx][j >> 2][u][j & 3]).value * acc[1][hx][j >> 2][u][j & 3];
+          };
+          if (p.act == QGTC_ACT_SILU) gates(QGTC_ACT_SILU);
+          else gates(QGTC_ACT_GELU);
+          top = abs_max(h[hx * 4 + u]);
+          if (p.out && m < p.rows) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int t = 2 * k + (j >> 2);
-              const float h = gate<false>(p.act, acc[0][hx][t][u][j & 3]).value * acc[1][hx][t][u][j & 3];
-              v[j] = whole || n0 + 8 * k + j < p.cols ? h : 0.0f;
-              acc[0][hx][t][u][j & 3] = v[j];
+            for (int k = 0; k < 2; ++k) {
+              float v[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = h[hx * 4 + u][8 * k + j];
+              store8(p.out, p.ld_out, m, n0 + 8 * k, v);
             }
-            top = max(top, abs_max(v));
-            if (p.out && m < p.rows) store8(p.out, p.ld_out, m, n0 + 8 * k, v);
           }
           top = max(top, (uint32_t)__shfl_xor((int)top, 16));
           top = max(top, (uint32_t)__shfl_xor((int)top, 32));
           if (g == 0) tops[wn * kTile + wm * 128 + hx * 64 + u * 16 + r] = top;
         }
       if (!p.codes) return;
-      __syncthreads();
+      meet_lds();
       uint32_t* const again = tops + 2 * kTile;
       uint32_t near = 0u;                                // 16 rows in which the exact largest value is wanted
 #pragma unroll
@@ -205,23 +217,29 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
         near |= __ballot(near_border(max(mine, tops[(wn ^ 1) * kTile + lr]))) ? 1u << i : 0u;
         if (g == 0) again[wn * kTile + lr] = mine;
       }
-#pragma unroll 1
-      for (; near; near &= near - 1u) {                  // (once, not for every 16 rows: the loop of products has to stay in the cache)
-        const int i = __ffs(near) - 1, lr = wm * 128 + i * 16 + r, m = m0 + lr;
-        const uint32_t top = max(tops[lr], tops[kTile + lr]), from = m < p.rows && near_border(top) ? border_from(top) : 0xffffffffu;
-        uint32_t want = 0u;
+      if (near) {
+        uint32_t want[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (j != i) continue;
+        for (int i = 0; i < 8; ++i) {
+          const int lr = wm * 128 + i * 16 + r;
+          const uint32_t top = max(tops[lr], tops[kTile + lr]), from = m0 + lr < p.rows && near_border(top) ? border_from(top) : 0xffffffffu;
+          want[i] = 0u;
 #pragma unroll
-          for (int k = 0; k < 16; ++k) want |= abs_bits(acc[0][j >> 2][k >> 2][j & 3][k & 3]) >= from ? 1u << k : 0u;
+          for (int j = 0; j < 16; ++j) want[i] |= abs_bits(h[i][j]) >= from ? 1u << j : 0u;
         }
-        uint32_t exact = exact_top(p, m, n0, want);
-        exact = max(exact, (uint32_t)__shfl_xor((int)exact, 16));
-        exact = max(exact, (uint32_t)__shfl_xor((int)exact, 32));
-        if (g == 0 && from != 0xffffffffu) again[wn * kTile + lr] = exact;
+#pragma unroll 1
+        for (; near; near &= near - 1u) {                // (once, not for every 16 rows: the loop of products has to stay in the cache)
+          const int i = __ffs(near) - 1, lr = wm * 128 + i * 16 + r;
+          uint32_t mine = 0u;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) mine = j == i ? want[j] : mine;
+          uint32_t exact = exact_top(p, m0 + lr, n0, mine);
+          exact = max(exact, (uint32_t)__shfl_xor((int)exact, 16));
+          exact = max(exact, (uint32_t)__shfl_xor((int)exact, 32));
+          if (g == 0 && near_border(max(tops[lr], tops[kTile + lr]))) again[wn * kTile + lr] = exact;
+        }
       }
-      __syncthreads();
+      meet_lds();
 #pragma unroll
       for (int hx = 0; hx < 2; ++hx)
 #pragma unroll
@@ -232,10 +250,15 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
             u32x4 c;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-              const v4f& v = acc[0][hx][t][u];
+              const float* const v = &h[hx * 4 + u][4 * t];
               c[t] = encode4(v[0], v[1], v[2], v[3], e);
-              const int left = p.cols - (n0 + 4 * t);
-              if (e == 255u && left < 4) c[t] &= left <= 0 ? 0u : 0xffffffffu >> (8 * (4 - left));   // (zeros past the end)
+            }
+            if (!whole && e == 255u) {                   // (zeros past the end, whatever the block)
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                const int left = p.cols - (n0 + 4 * t);
+                if (left < 4) c[t] &= left <= 0 ? 0u : 0xffffffffu >> (8 * (4 - left));
+              }
             }
             *reinterpret_cast<u32x4*>(p.codes + (int64_t)m * p.ld_codes + n0) = c;
             if (g == 0 && wn == 0) p.scales[(int64_t)m * p.ld_scales + bn] = (uint8_t)e;
@@ -244,6 +267,15 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
       // (the next tile's largest values are written a barrier of its products later)
     } else {
       const int n0 = bn * TN + wn * 64 + 8 * g;
+      // (all of dh at once: each load that is waited for waits for the next tile's operands as well)
+      u32x4 dh_bits[8][2];
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int m = min(m0 + wm * 128 + (i >> 1) * 16 + r, p.rows - 1);
+          dh_bits[i >> 1][i & 1] = *reinterpret_cast<const u32x4_any*>((const T*)p.dh + (int64_t)m * p.ld_dh + n0 + 32 * (i & 1));
+        }
+      }
 #pragma unroll
       for (int hx = 0; hx < 2; ++hx)
 #pragma unroll
@@ -254,15 +286,27 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
             for (int k = 0; k < 2; ++k) {
               const int n = n0 + 32 * k;
               float dh[8], dg[8], du[8];
-              if (p.type == QGTC_F16) load8_of<QGTC_F16>((const uint16_t*)p.dh + (int64_t)m * p.ld_dh, n, p.cols, dh);
-              else load8_of<QGTC_BF16>((const uint16_t*)p.dh + (int64_t)m * p.ld_dh, n, p.cols, dh);
+              if (whole) {
 #pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const int t = 2 * k + (j >> 2);
-                const Gate v = gate<false>(p.act, acc[0][hx][t][u][j & 3]);
-                dg[j] = dh[j] * acc[1][hx][t][u][j & 3] * v.slope;
-                du[j] = dh[j] * v.value;
+                for (int j = 0; j < 4; ++j) {
+                  const f32x2 v = Half<TYPE>::wide(dh_bits[hx * 4 + u][k][j]);
+                  dh[2 * j] = v.x;
+                  dh[2 * j + 1] = v.y;
+                }
+              } else {
+                load8_of<TYPE>((const T*)p.dh + (int64_t)m * p.ld_dh, n, p.cols, dh);
               }
+              auto gates = [&](int act) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const int t = 2 * k + (j >> 2);
+                  const Gate v = gate<false>(act, acc[0][hx][t][u][j & 3]);
+                  dg[j] = dh[j] * acc[1][hx][t][u][j & 3] * v.slope;
+                  du[j] = dh[j] * v.value;
+                }
+              };
+              if (p.act == QGTC_ACT_SILU) gates(QGTC_ACT_SILU);
+              else gates(QGTC_ACT_GELU);
               store8(p.out, p.ld_out, m, n, dg);
               store8(p.out2, p.ld_out2, m, n, du);
             }
@@ -324,6 +368,14 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
   meet<0>();                                           // (nothing is on its way to LDS any more)
 }
 
+template <int MODE, int TYPE>
+qgtc_status launch(const TileParams& t, unsigned workgroups, hipStream_t stream) {
+  static OncePerDevice once;
+  if (!allow_lds(once, reinterpret_cast<const void*>(&tile_kernel<MODE, TYPE>), kTileLds)) return QGTC_ERR_HIP;
+  hipLaunchKernelGGL((tile_kernel<MODE, TYPE>), dim3(workgroups), dim3(256), kTileLds, stream, t);
+  return launch_status();
+}
+
 }  // namespace
 
 template <int MODE>
@@ -333,13 +385,9 @@ qgtc_status launch_tiles(const ProductParams& p, hipStream_t stream) {
   t.tiles_m = (uint32_t)cdiv(p.rows, kTile);
   t.tiles_n = (uint32_t)cdiv(p.cols, MODE == kProduct ? kTile : kTile / 2);
   t.per_group = 8u * t.tiles_n;
-  const int64_t tiles = (int64_t)t.tiles_m * t.tiles_n;
-  t.per_xcd = (uint32_t)cdiv(tiles, 8);
+  t.per_xcd = (uint32_t)cdiv((int64_t)t.tiles_m * t.tiles_n, 8);
   const uint32_t most = (uint32_t)(device_compute_units() / 8), workgroups = 8u * (t.per_xcd < most ? t.per_xcd : most);
-  static OncePerDevice once;
-  if (!allow_lds(once, reinterpret_cast<const void*>(&tile_kernel<MODE>), kTileLds)) return QGTC_ERR_HIP;
-  hipLaunchKernelGGL(tile_kernel<MODE>, dim3(workgroups), dim3(256), kTileLds, stream, t);
-  return launch_status();
+  return p.type == QGTC_F16 ? launch<MODE, QGTC_F16>(t, workgroups, stream) : launch<MODE, QGTC_BF16>(t, workgroups, stream);
 }
 template qgtc_status launch_tiles<kProduct>(const ProductParams& p, hipStream_t stream);
 template qgtc_status launch_tiles<kGated>(const ProductParams& p, hipStream_t stream);
