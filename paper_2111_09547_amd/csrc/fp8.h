@@ -112,6 +112,38 @@ __device__ __forceinline__ void store8_of(typename Float<TYPE>::type* row, int c
   }
 }
 
+// The same, kept as they come from memory until they are wanted.
+template <int TYPE> struct Raw8 {
+  u32x4 v;
+  __device__ __forceinline__ void load(const uint16_t* row, int c, int cols) {
+    if (c + 8 <= cols) {
+      v = *reinterpret_cast<const u32x4_any*>(row + c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = c + 2 * i < cols ? row[c + 2 * i] : 0u, hi = c + 2 * i + 1 < cols ? row[c + 2 * i + 1] : 0u;
+        v[i] = lo | hi << 16;
+      }
+    }
+  }
+  __device__ __forceinline__ void widen(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x2 w = Half<TYPE>::wide(v[i]);
+      f[2 * i] = w.x;
+      f[2 * i + 1] = w.y;
+    }
+  }
+};
+template <> struct Raw8<QGTC_F32> {
+  float v[8];
+  __device__ __forceinline__ void load(const float* row, int c, int cols) { load8_of<QGTC_F32>(row, c, cols, v); }
+  __device__ __forceinline__ void widen(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = v[i];
+  }
+};
+
 // The largest absolute value of a block goes as its bits: among floats without a sign these order as the values do,
 // infinities and NaN above all others.
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }

@@ -1,6 +1,7 @@
 // Root-mean-square norm with the residual's addition and output in 8-bit floats, and its gradients.
 //
-// Both are bound by memory: forward, of a bf16 row with residual, 6 bytes read and written and one of codes per entry.  A row's
+// Both are bound by memory: forward, of a bf16 row with residual, 6 bytes read and written and one of codes per entry (8192 x 4096 43 us,
+// 5.5 TB/s, a copy's rate).  A row's
 // entries stay in registers from the load to the codes, so everything is read once: a lane has V pieces of 8 consecutive
 // entries, 16 lanes a block of 128, and a row is shared by as many waves as it takes (one wave: no LDS, four rows a workgroup).
 #include "fp8.h"
@@ -91,6 +92,9 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_kernel(const NormParams
   }
 }
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+__host__ __device__ inline int64_t sum_pitch(int cols) { return ((int64_t)cols + 3) / 4 * 4; }   // of a group's share of dweight
+
 struct GradParams {
   const void *dy, *sum, *weight, *dsum;
   const float* rstd;
@@ -101,7 +105,8 @@ struct GradParams {
 };
 
 // A workgroup takes every groups-th row (ONE: four times as many rows, a wave each) and keeps its share of dweight in
-// registers; groups' shares are added up in order by the second kernel, so the result does not depend on timing.
+// registers; groups' shares are added up in order by the second kernel, so the result does not depend on timing.  The next row
+// is on its way while one is worked on, where registers have room for it (8192 x 4096 bf16: 65 us without, 52 with, 5.1 TB/s).
 template <int TYPE, int V, bool ONE>
 __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_grad_kernel(const GradParams p) {
   typedef typename Float<TYPE>::type T;
@@ -110,45 +115,66 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_grad_kernel(const GradP
   const int wave = (int)(threadIdx.x >> 6), lane = (int)(threadIdx.x & 63u);
   const int c0 = (ONE ? 0 : wave * V * kPiece) + lane * 8;
   const int64_t step = (int64_t)p.groups * (ONE ? 4 : 1);
+  constexpr bool ROOM = ONE || V == 1;             // in registers, for the weight and the next row
   float w[V][8], dw[V][8];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    load_weight8(p.weight, p.weight_type, c0 + i * kPiece, p.cols, w[i]);
+    if (ROOM) load_weight8(p.weight, p.weight_type, c0 + i * kPiece, p.cols, w[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
   }
-  int turn = 0;
-  for (int64_t row = ONE ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x; row < p.rows; row += step) {
-    float dy[V][8], s[V][8], ds[V][8];
+  struct Row {
+    Raw8<TYPE> dy[V], s[V], ds[V];
+    float rstd;
+  };
+  auto load = [&](int64_t row, Row& to) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      load8_of<TYPE>((const T*)p.dy + row * p.ld_dy, c0 + i * kPiece, p.cols, dy[i]);
-      load8_of<TYPE>((const T*)p.sum + row * p.ld_sum, c0 + i * kPiece, p.cols, s[i]);
-      if (p.dsum) load8_of<TYPE>((const T*)p.dsum + row * p.ld_dsum, c0 + i * kPiece, p.cols, ds[i]);
+      to.dy[i].load((const T*)p.dy + row * p.ld_dy, c0 + i * kPiece, p.cols);
+      to.s[i].load((const T*)p.sum + row * p.ld_sum, c0 + i * kPiece, p.cols);
+      if (p.dsum) to.ds[i].load((const T*)p.dsum + row * p.ld_dsum, c0 + i * kPiece, p.cols);
     }
-    const float rstd = p.rstd[row];
+    to.rstd = p.rstd[row];
+  };
+  int64_t row = ONE ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
+  Row now, then;
+  if (ROOM && row < p.rows) load(row, now);
+  int turn = 0;
+  for (; row < p.rows; row += step) {
+    if (!ROOM) load(row, now);
+    else if (row + step < p.rows) load(row + step, then);
+    float dy[V][8], s[V][8];
+    const float rstd = now.rstd;
     float along = 0.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
+    for (int i = 0; i < V; ++i) {
+      now.dy[i].widen(dy[i]);
+      now.s[i].widen(s[i]);
+      if (!ROOM) load_weight8(p.weight, p.weight_type, c0 + i * kPiece, p.cols, w[0]);
+      const float(&wi)[8] = w[ROOM ? i : 0];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         s[i][j] = s[i][j] * rstd;                  // hat
         dw[i][j] = fmaf(dy[i][j], s[i][j], dw[i][j]);
-        dy[i][j] = dy[i][j] * w[i][j];             // g
+        dy[i][j] = dy[i][j] * wi[j];               // g
         along = fmaf(dy[i][j], s[i][j], along);
       }
+    }
     // (two boxes in turn: a wave that is a row ahead does not write where another still reads)
     const float mean = row_sum<ONE>(along, part[turn]) / (float)p.cols;
     turn ^= 1;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
+      float ds[8];
+      if (p.dsum) now.ds[i].widen(ds);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float d = rstd * (dy[i][j] - s[i][j] * mean);
-        dy[i][j] = p.dsum ? d + ds[i][j] : d;
+        dy[i][j] = p.dsum ? d + ds[j] : d;
       }
       store8_of<TYPE>((T*)p.dx + row * p.ld_dx, c0 + i * kPiece, p.cols, dy[i]);
     }
+    if (ROOM) now = then;
   }
   if (!p.partial) return;
   if constexpr (ONE) {
@@ -168,26 +194,32 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_grad_kernel(const GradP
         for (int j = 0; j < 8; ++j) dw[i][j] += box[(k * V + i) * kPiece + j * 64 + lane];
   }
 #pragma unroll
-  for (int i = 0; i < V; ++i) store8_of<QGTC_F32>(p.partial + (int64_t)blockIdx.x * p.cols, c0 + i * kPiece, p.cols, dw[i]);
+  for (int i = 0; i < V; ++i) store8_of<QGTC_F32>(p.partial + (int64_t)blockIdx.x * sum_pitch(p.cols), c0 + i * kPiece, p.cols, dw[i]);
 }
 
-// Eight columns of the groups' shares: a thread adds up the shares of every 32nd group, four loads ahead of the sum, and the threads'
-// sums are added in order.
-constexpr int kSumColumns = 8;
+// 32 columns of the groups' shares: a thread adds up four columns of every 32nd share, and the threads' sums are added in order.
 __global__ __launch_bounds__(256) void norm_grad_sum_kernel(const float* partial, float* dweight, int cols, int groups) {
-  __shared__ float box[32][kSumColumns + 1];
-  const int c = (int)blockIdx.x * kSumColumns + (int)(threadIdx.x & 7u), k = (int)(threadIdx.x >> 3);
-  float s = 0.0f;
-  if (c < cols) {
-#pragma unroll 4
-    for (int g = k; g < groups; g += 32) s += partial[(int64_t)g * cols + c];
-  }
-  box[k][threadIdx.x & 7u] = s;
-  __syncthreads();
-  if (k == 0 && c < cols) {
+  __shared__ float box[32][33];
+  const int q = (int)(threadIdx.x & 7u) * 4, k = (int)(threadIdx.x >> 3), c = (int)blockIdx.x * 32 + q;
+  const int64_t pitch = sum_pitch(cols);
+  f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (c < pitch) {
+#pragma unroll 8
+    for (int g = k; g < groups; g += 32) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(partial + (int64_t)g * pitch + c);
 #pragma unroll
-    for (int i = 1; i < 32; ++i) s += box[i][threadIdx.x & 7u];
-    dweight[c] = s;
+      for (int i = 0; i < 4; ++i) s[i] += v[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) box[k][q + i] = s[i];
+  __syncthreads();
+  const int col = (int)blockIdx.x * 32 + (int)threadIdx.x;
+  if (threadIdx.x < 32 && col < cols) {
+    float sum = box[0][threadIdx.x];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) sum += box[i][threadIdx.x];
+    dweight[col] = sum;
   }
 }
 
@@ -208,9 +240,11 @@ qgtc_status launch_norm(const NormParams& p, hipStream_t stream) {
   return v == 2 ? launch_norm<TYPE, 2, false>(p, stream) : launch_norm<TYPE, 4, false>(p, stream);
 }
 
+// Up to 1024 columns a wave has a row to itself and no barriers (8192 x 1024 bf16: two waves a row without the next one 33.8 us, so 17.2;
+// at 2048 columns one wave loses to four, 24.6 and 19.4).
+constexpr int kOneWave = 1024;
 int grad_groups(int rows, int cols) {
-  const int per = cols <= kPiece ? 4 : 1;          // rows that a workgroup has at once
-  const int64_t most = cdiv(rows, per), groups = 512;
+  const int64_t most = cdiv(rows, cols <= kOneWave ? 4 : 1), groups = 2 * device_compute_units();
   return (int)(most < groups ? most : groups);
 }
 template <int TYPE, int V, bool ONE>
@@ -223,6 +257,7 @@ qgtc_status launch_grad(const GradParams& p, hipStream_t stream) {
 template <int TYPE>
 qgtc_status launch_grad(const GradParams& p, hipStream_t stream) {
   if (p.cols <= kPiece) return launch_grad<TYPE, 1, true>(p, stream);
+  if (p.cols <= kOneWave) return launch_grad<TYPE, 2, true>(p, stream);
   const int v = pieces(p.cols);
   if (v == 1) return launch_grad<TYPE, 1, false>(p, stream);
   return v == 2 ? launch_grad<TYPE, 2, false>(p, stream) : launch_grad<TYPE, 4, false>(p, stream);
@@ -277,7 +312,7 @@ extern "C" qgtc_status qgtc_rms_norm(const qgtc_norm* n, void* stream) {
 
 extern "C" size_t qgtc_rms_norm_backward_workspace_bytes(int32_t rows, int32_t cols) {
   if (rows <= 0 || cols <= 0 || cols > qgtc::kMostColumns) return 0;
-  return (size_t)qgtc::grad_groups(rows, cols) * (size_t)cols * 4;
+  return (size_t)qgtc::grad_groups(rows, cols) * (size_t)qgtc::sum_pitch(cols) * 4;
 }
 
 extern "C" qgtc_status qgtc_rms_norm_backward(const qgtc_norm_grad* n, void* workspace, size_t workspace_bytes, void* stream) {
@@ -328,6 +363,6 @@ extern "C" qgtc_status qgtc_rms_norm_backward(const qgtc_norm_grad* n, void* wor
     st = n->type == QGTC_F32 ? launch_grad<QGTC_F32>(p, s) : n->type == QGTC_F16 ? launch_grad<QGTC_F16>(p, s) : launch_grad<QGTC_BF16>(p, s);
     if (st != QGTC_OK || !n->dweight) return st;
   }
-  hipLaunchKernelGGL(norm_grad_sum_kernel, dim3((unsigned)cdiv(n->cols, kSumColumns)), dim3(256), 0, s, p.partial, n->dweight, n->cols, p.groups);
+  hipLaunchKernelGGL(norm_grad_sum_kernel, dim3((unsigned)cdiv(n->cols, 32)), dim3(256), 0, s, p.partial, n->dweight, n->cols, p.groups);
   return launch_status();
 }
