@@ -79,14 +79,15 @@ __global__ __launch_bounds__(256, 1) void mid_kernel(const MidParams mp) {
     uint32_t sx[4], sw[4];
   };
   const uint32_t lane_at = (uint32_t)r * kBlock + (uint32_t)((g ^ (r & 7)) * 16);
+  const uint32_t sx_at = (uint32_t)(kScales + (wm * 64 + r) * 4), sw_at = (uint32_t)(kScales + (kSide + wn * 64 + r) * 4);
   auto read = [&](int k, Block& b, int t) {          // a quarter of them
-    const uint32_t at = (uint32_t)(k & 3) * kBuffer, s_at = kScales + (uint32_t)(k >> 2 & 1) * kSlot + (uint32_t)(k & 3);
+    const uint32_t at = (uint32_t)(k & 3) * kBuffer, s_at = (uint32_t)(k >> 2 & 1) * kSlot + (uint32_t)(k & 3);
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
       const uint8_t* const from = lds + o * kOperand + ((o ? wn : wm) * 64 + t * 16) * kBlock;
       const v4i lo = *reinterpret_cast<const v4i*>(from + (at + lane_at)), hi = *reinterpret_cast<const v4i*>(from + (at + (lane_at ^ 64u)));
       (o ? b.w : b.x)[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      (o ? b.sw : b.sx)[t] = lds[s_at + o * (kSide * 4) + ((o ? wn : wm) * 64 + t * 16 + r) * 4];
+      (o ? b.sw : b.sx)[t] = lds[(o ? sw_at : sx_at) + s_at + (uint32_t)(t * 64)];
     }
   };
   v4f acc[4][4];                                     // [w][x]

@@ -119,8 +119,9 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
     const v4i a = *reinterpret_cast<const v4i*>(at + (buffer + lane_at)), b = *reinterpret_cast<const v4i*>(at + (buffer + (lane_at ^ 64u)));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   };
+  const uint32_t sx_at = (uint32_t)(kScales + (wm * 128 + r) * 4), sw_at = (uint32_t)(kScales + (kTile + wn * 128 + r) * 4);
   auto read_scale = [&](uint32_t at, int operand, int half, int t) -> uint32_t {   // at: slot and byte
-    return lds[kScales + at + operand * (kTile * 4) + ((operand ? wn : wm) * 128 + half * 64 + t * 16) * 4 + r * 4];
+    return lds[(operand ? sw_at : sx_at) + at + (uint32_t)((half * 64 + t * 16) * 4)];
   };
 
   v4f acc[2][2][4][4];                                 // [half of w][half of x][w][x]
