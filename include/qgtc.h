@@ -707,6 +707,8 @@ qgtc_status qgtc_fold_batchnorm(const double* gamma, const double* beta, const d
  * the nearest e4m3, ties to even.  A block with an infinity or a NaN has e = 255 and NaN codes:
  * all of its values are NaN.
  *
+ * A matrix has at most 2^29 rows and columns (QGTC_ERR_SHAPE).
+ *
  * Other tensors are row-major in one of three types, with a leading dimension in elements
  * (any that is at least the number of columns) and the alignment of their type.
  * ------------------------------------------------------------------------- */

@@ -7,7 +7,8 @@
 namespace qgtc {
 
 constexpr int kBlock = 128;                        // entries that share a scale
-constexpr int kMostEntries = 1 << 30;              // rows, and columns, of one matrix
+constexpr int kMostEntries = 1 << 29;              // rows, and columns, of one matrix
+constexpr int64_t kMostThreads = (int64_t)1 << 31; // of a launch along an axis (their number has 32 bits): what is more takes several
 
 inline int fp8_blocks(int cols) { return cdiv(cols, kBlock); }
 qgtc_status check_fp8(const qgtc_fp8* m);          // fp8.hip

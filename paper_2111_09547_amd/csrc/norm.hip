@@ -228,9 +228,23 @@ int pieces(int cols) { return cols <= 8192 ? 1 : cols <= 16384 ? 2 : 4; }
 
 template <int TYPE, int V, bool ONE>
 qgtc_status launch_norm(const NormParams& p, hipStream_t stream) {
+  typedef typename Float<TYPE>::type T;
   const int waves = ONE ? 4 : cdiv(p.cols, V * kPiece);
-  hipLaunchKernelGGL((norm_kernel<TYPE, V, ONE>), dim3((unsigned)(ONE ? cdiv(p.rows, 4) : p.rows)), dim3(64u * (unsigned)waves), 0, stream, p);
-  return launch_status();
+  const int64_t most = kMostThreads / (ONE ? 64 : 64 * waves) / 4 * 4;
+  for (int64_t r0 = 0; r0 < p.rows; r0 += most) {
+    NormParams q = p;
+    q.rows = (int32_t)(p.rows - r0 < most ? p.rows - r0 : most);
+    q.x = (const T*)p.x + r0 * p.ld_x;
+    if (p.residual) q.residual = (const T*)p.residual + r0 * p.ld_residual;
+    if (p.sum) q.sum = (T*)p.sum + r0 * p.ld_sum;
+    if (p.y) q.y = (T*)p.y + r0 * p.ld_y;
+    if (p.rstd) q.rstd = p.rstd + r0;
+    if (p.codes) q.codes = p.codes + r0 * p.ld_codes, q.scales = p.scales + r0 * p.ld_scales;
+    hipLaunchKernelGGL((norm_kernel<TYPE, V, ONE>), dim3((unsigned)(ONE ? cdiv(q.rows, 4) : q.rows)), dim3(64u * (unsigned)waves), 0, stream, q);
+    const qgtc_status st = launch_status();
+    if (st != QGTC_OK) return st;
+  }
+  return QGTC_OK;
 }
 template <int TYPE>
 qgtc_status launch_norm(const NormParams& p, hipStream_t stream) {

@@ -29,7 +29,8 @@ struct ProductParams {
   int64_t ld_out;
   void* out2;                // du
   int64_t ld_out2;
-  float* wide;               // h in fp32, rows x cols
+  float* wide;               // h in fp32
+  int64_t ld_wide;
   const void* dh;
   int64_t ld_dh;
   uint8_t* codes;            // h in 8-bit floats

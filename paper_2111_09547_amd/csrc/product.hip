@@ -103,7 +103,7 @@ __global__ __launch_bounds__(512) void few_kernel(const ProductParams p) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) a[k] = gate<true>(p.act, sum[0][k]).value * sum[D - 1][k];
       if (p.out) store4_as(p.type, p.out, (int64_t)m * p.ld_out + n, left, a);
-      if (p.wide) store4_of<QGTC_F32>(p.wide, (int64_t)m * p.cols + n, left, a);
+      if (p.wide) store4_of<QGTC_F32>(p.wide, (int64_t)m * p.ld_wide + n, left, a);
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -123,22 +123,27 @@ qgtc_status launch_few(const ProductParams& p, hipStream_t stream) {
   constexpr int D = MODE == kProduct ? 1 : 2;
   const int waves = 8;
   const size_t lds = (size_t)waves * D * MT * 64 * 16;
-  // (a launch has at most 65535 workgroups along the second axis: rows beyond go in launches of their own)
-  const int most = 65535 * 16 * MT;
-  for (int64_t m0 = 0; m0 < p.rows; m0 += most) {
-    ProductParams q = p;
-    q.rows = (int32_t)(p.rows - m0 < most ? p.rows - m0 : most);
-    q.x.codes += m0 * p.x.ld;
-    q.x.scales += m0 * p.x.ld_scales;
-    const int64_t b = float_bytes(p.type);
-    if (q.out) q.out = (char*)p.out + m0 * p.ld_out * b;
-    if (q.out2) q.out2 = (char*)p.out2 + m0 * p.ld_out2 * b;
-    if (q.dh) q.dh = (const char*)p.dh + m0 * p.ld_dh * b;
-    if (q.wide) q.wide += m0 * p.cols;
-    hipLaunchKernelGGL((few_kernel<MODE, MT, WIDE>), dim3((unsigned)cdiv(p.cols, 16), (unsigned)cdiv(q.rows, 16 * MT)), dim3(64u * waves), lds, stream, q);
-    const qgtc_status st = launch_status();
-    if (st != QGTC_OK) return st;
-  }
+  // (what is beyond a launch's size goes in launches of its own: 65535 workgroups along the second axis)
+  const int most = 65535 * 16 * MT, most_cols = (int)(kMostThreads / (64 * waves) * 16);
+  const int64_t b = float_bytes(p.type);
+  for (int64_t m0 = 0; m0 < p.rows; m0 += most)
+    for (int64_t n0 = 0; n0 < p.cols; n0 += most_cols) {
+      ProductParams q = p;
+      q.rows = (int32_t)(p.rows - m0 < most ? p.rows - m0 : most);
+      q.cols = (int32_t)(p.cols - n0 < most_cols ? p.cols - n0 : most_cols);
+      q.x.codes += m0 * p.x.ld;
+      q.x.scales += m0 * p.x.ld_scales;
+      q.w.codes += n0 * p.w.ld;
+      q.w.scales += n0 * p.w.ld_scales;
+      if (D == 2) q.u.codes += n0 * p.u.ld, q.u.scales += n0 * p.u.ld_scales;
+      if (q.out) q.out = (char*)p.out + (m0 * p.ld_out + n0) * b;
+      if (q.out2) q.out2 = (char*)p.out2 + (m0 * p.ld_out2 + n0) * b;
+      if (q.dh) q.dh = (const char*)p.dh + (m0 * p.ld_dh + n0) * b;
+      if (q.wide) q.wide += m0 * p.ld_wide + n0;
+      hipLaunchKernelGGL((few_kernel<MODE, MT, WIDE>), dim3((unsigned)cdiv(q.cols, 16), (unsigned)cdiv(q.rows, 16 * MT)), dim3(64u * waves), lds, stream, q);
+      const qgtc_status st = launch_status();
+      if (st != QGTC_OK) return st;
+    }
   return QGTC_OK;
 }
 
@@ -150,12 +155,12 @@ qgtc_status launch_few(const ProductParams& p, hipStream_t stream) {
 }
 
 // h from memory into 8-bit floats: 16 lanes have a block, a wave 512 columns of a row.
-__global__ __launch_bounds__(256) void gated_rows_kernel(const ProductParams p, uint32_t groups) {
-  const uint32_t unit = blockIdx.x * 4u + (threadIdx.x >> 6);
-  const int m = (int)(unit / groups), c = (int)(unit % groups) * 512 + (int)(threadIdx.x & 63u) * 8;
+__global__ __launch_bounds__(256) void gated_rows_kernel(const ProductParams p, uint32_t groups, int64_t first) {
+  const int64_t unit = first + blockIdx.x * 4u + (threadIdx.x >> 6);
+  const int m = (int)(unit / groups), c = (int)(unit - (int64_t)m * groups) * 512 + (int)(threadIdx.x & 63u) * 8;
   if (m >= p.rows) return;
   float v[8];
-  load8_of<QGTC_F32>(p.wide + (int64_t)m * p.cols, c, p.cols, v);
+  load8_of<QGTC_F32>(p.wide + (int64_t)m * p.ld_wide, c, p.cols, v);
   uint32_t top = max_of_16_lanes(abs_max(v));
   const bool near = near_border(top);
   if (__ballot(near)) {
@@ -291,6 +296,7 @@ extern "C" qgtc_status qgtc_fp8_gated(const qgtc_fp8* X, const qgtc_fp8* G, cons
       if (((uintptr_t)workspace & 15u) != 0) return QGTC_ERR_ALIGN;
       if (workspace_bytes < need) return QGTC_ERR_WORKSPACE;
       p.wide = reinterpret_cast<float*>(workspace);
+      p.ld_wide = p.cols;
     }
     p.codes = out->codes;
     p.scales = out->scales;
@@ -304,8 +310,13 @@ extern "C" qgtc_status qgtc_fp8_gated(const qgtc_fp8* X, const qgtc_fp8* G, cons
   if (from_h) return quantize_rows(h, QGTC_F32, p.rows, p.cols, ld_h, *out, s);
   if (!p.wide) return QGTC_OK;
   const uint32_t groups = (uint32_t)cdiv(p.cols, 512);
-  hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)(((int64_t)groups * p.rows + 3) / 4)), dim3(256), 0, s, p, groups);
-  return launch_status();
+  const int64_t units = (int64_t)groups * p.rows;
+  for (int64_t first = 0; first < units && st == QGTC_OK; first += kMostThreads / 64) {
+    const int64_t here = units - first < kMostThreads / 64 ? units - first : kMostThreads / 64;
+    hipLaunchKernelGGL(gated_rows_kernel, dim3((unsigned)((here + 3) / 4)), dim3(256), 0, s, p, groups, first);
+    st = launch_status();
+  }
+  return st;
 }
 
 extern "C" qgtc_status qgtc_fp8_gated_backward(const qgtc_fp8* X, const qgtc_fp8* G, const qgtc_fp8* U, int32_t act,

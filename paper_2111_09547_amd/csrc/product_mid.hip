@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256, 1) void mid_kernel(const MidParams mp) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[0][j] = gate<WIDE>(p.act, v[0][j]).value * v[1][j];
       if (p.out) store8_as<WIDE>(p.type, p.out, p.ld_out, m, n, p.cols, v[0]);
-      if (p.wide) store8_of<QGTC_F32>(p.wide + (int64_t)m * p.cols, n, p.cols, v[0]);
+      if (p.wide) store8_of<QGTC_F32>(p.wide + (int64_t)m * p.ld_wide, n, p.cols, v[0]);
     } else {
       const int n = n0 + wn * 32 + 8 * g;
       float dh[8], dg[8], du[8];

@@ -31,6 +31,7 @@ struct QuantizeParams {
   uint8_t* scales;
   int64_t ld_codes, ld_scales;
   uint32_t groups;           // along a row: of 512 columns
+  int64_t first;             // of the launch's units
 };
 
 // Along rows: 16 lanes have a block, a wave 512 columns of a row, and ROWS of those at a time.
@@ -38,10 +39,9 @@ constexpr int kQuantRows = 4;
 template <int TYPE>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeParams p) {
   typedef typename Float<TYPE>::type T;
-  const uint32_t unit = blockIdx.x * 4u + (threadIdx.x >> 6);
-  const uint32_t rg = unit / p.groups;
+  const int64_t unit = p.first + blockIdx.x * 4u + (threadIdx.x >> 6), rg = unit / p.groups;
   const int c = (int)(unit - rg * p.groups) * 512 + (int)(threadIdx.x & 63u) * 8;
-  const int64_t row0 = (int64_t)rg * kQuantRows;
+  const int64_t row0 = rg * kQuantRows;
   float v[kQuantRows][8];
 #pragma unroll
   for (int i = 0; i < kQuantRows; ++i)
@@ -106,8 +106,13 @@ template <int TYPE>
 qgtc_status launch_rows(QuantizeParams p, hipStream_t stream) {
   p.groups = (uint32_t)cdiv(p.cols, 512);
   const int64_t units = (int64_t)p.groups * cdiv(p.rows, kQuantRows);
-  hipLaunchKernelGGL(quantize_rows_kernel<TYPE>, dim3((unsigned)((units + 3) / 4)), dim3(256), 0, stream, p);
-  return launch_status();
+  for (p.first = 0; p.first < units; p.first += kMostThreads / 64) {
+    const int64_t here = units - p.first < kMostThreads / 64 ? units - p.first : kMostThreads / 64;
+    hipLaunchKernelGGL(quantize_rows_kernel<TYPE>, dim3((unsigned)((here + 3) / 4)), dim3(256), 0, stream, p);
+    const qgtc_status st = launch_status();
+    if (st != QGTC_OK) return st;
+  }
+  return QGTC_OK;
 }
 
 template <int TYPE>

@@ -66,8 +66,8 @@ def test_quantize_refuses(b, columns):
     bad.ld_scales = 0
     assert call(dst=bad) == SHAPE
     big = form(b, 1, 1)
-    big.rows, big.cols, big.ld = (1, (1 << 30) + 1, 1 << 31)
-    assert f(0x30000, 0, 1, (1 << 30) + 1, 1 << 31, 0, C.byref(big), None) == SHAPE
+    big.rows, big.cols, big.ld = (1, (1 << 29) + 1, 1 << 30)
+    assert f(0x30000, 0, 1, (1 << 29) + 1, 1 << 30, 0, C.byref(big), None) == SHAPE
     assert call(rows=0, src=None) == OK
 
 

@@ -294,6 +294,31 @@ def test_offsets_past_32_bits(rows):
     assert (U.raw(m.codes) == codes).all() and (U.raw(m.scales)[:, :3] == scales).all()
 
 
+def test_norm_offsets_past_32_bits():
+    rows, cols, ld = 300, 200, 1 << 23
+    buf = torch.empty((rows, ld), dtype=torch.bfloat16, device="cuda")          # 5 GB: everything in columns of it
+    x, res, total, dy, dx = (buf[:, 1000 * k:1000 * k + cols] for k in range(5))
+    a, b, c = (U.activations(rows, cols, k).bfloat16().cuda() for k in (1, 2, 3))
+    x.copy_(a), res.copy_(b), dy.copy_(c)
+    w = torch.ones(cols, device="cuda")
+    n, want = q.qgtc_rms_norm(x, w, residual=res, sum_out=total, rstd=True), q.qgtc_rms_norm(a, w, residual=b, rstd=True)
+    assert torch.equal(total, want.sum) and (U.raw(n.fp8.codes) == U.raw(want.fp8.codes)).all()
+    got, dw = q.qgtc_rms_norm_backward(dy, total, w, n.rstd, out=dx)
+    dx2, dw2 = q.qgtc_rms_norm_backward(c, want.sum, w, want.rstd)
+    assert torch.equal(got, dx2) and torch.equal(dw, dw2)
+
+
+def test_more_rows_than_a_launch_takes():
+    rows = (1 << 25) + 70                                  # 64 lanes a row: 2^31 and some
+    x = torch.ones((rows, 1), dtype=torch.bfloat16, device="cuda")
+    x[-1], x[1 << 25], x[(1 << 25) - 1] = 3.0, 5.0, 7.0
+    n = q.qgtc_rms_norm(x, torch.full((1,), 2.0, device="cuda"), eps=0.0, fp8=False, y=True, rstd=True)
+    assert bool((n.y == 2.0).all()) and n.rstd[-1].item() == pytest.approx(1 / 3) and n.rstd[1 << 25].item() == pytest.approx(0.2)
+    m = q.qgtc_fp8_quantize(x)                             # four rows a wave: one launch, of 4 GB of codes
+    tail = m.codes[-80:, :1].float() * m.scales[-80:, :1].float()
+    assert torch.equal(tail, x[-80:].float()) and bool((m.codes[:, 1:].view(torch.uint8) == 0).all())
+
+
 # ---- the gated block ------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("rows", ROWS)
