@@ -351,6 +351,116 @@ def test_gated_and_its_gradients(act, rows, cols, inner):
             U.close(got[:, at:at + cols], want, np.abs(d) * tf * 1.01 + 2.0 ** -23 * np.abs(want) + U.rounded_tol(want, dtype), (at, dtype))
 
 
+# ---- the same at sizes that larger tiles are taken for: 128 x 128 and 256 x 256 by their number (a round of tiles per 256 compute
+# units), ragged at every edge, of one, two, odd and many blocks.  In 64 bits on the device.
+LARGE = [(300, 4100, 2050), (1000, 2056, 4100), (700, 8190, 100), (513, 4099, 260),              # 128 x 128
+         (8190, 4090, 1100), (8100, 8200, 520), (4090, 8190, 2048), (8192, 8192, 640), (3333, 8190, 3000)]   # 256 x 256
+GATED = [(300, 2050, 2050), (1000, 1030, 1030), (130, 4090, 260),
+         (4090, 4090, 1100), (4090, 8190, 100), (4090, 8190, 200), (2048, 8192, 1152), (2500, 5000, 2100)]
+
+
+def on_device(rows, cols, inner, seeds):
+    made = []
+    for (n, seed) in ((rows, seeds[0]),) + tuple((cols, s) for s in seeds[1:]):
+        t = U.activations(n, inner, seed) if seed == seeds[0] else U.weights(n, inner, seed)
+        m = q.qgtc_fp8_quantize(t.cuda())
+        wide = m.codes.double() * m.scales[:, :m.blocks].double().repeat_interleave(128, 1)
+        made.append((m, wide[:, :inner].contiguous()))
+    return made
+
+
+def device_tol(x, w, exact_products):
+    """U.product_tol of device matrices."""
+    blocks = -(-x.shape[1] // 128)
+    tol = (blocks + 128) * 2.0 ** -23 * (x.abs() @ w.abs().t().contiguous())
+    if not exact_products:
+        def tops(v):
+            return torch.nn.functional.pad(v.abs(), (0, -v.shape[1] % 8)).view(v.shape[0], -1, 8).amax(2)
+        tol = tol + 7 * 2.0 ** -13 * (tops(x) @ tops(w).t().contiguous())
+    return tol * 1.01
+
+
+def device_close(got, want, tol):
+    bad = (got.double() - want).abs() > tol + want.abs() * U.HALF[got.dtype] + U.TINY[got.dtype]
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist())
+
+
+@pytest.mark.parametrize("rows,cols,inner", LARGE)
+def test_large_product(rows, cols, inner):
+    (X, x), (W, w) = on_device(rows, cols, inner, (1, 2))
+    want = x @ w.t().contiguous()
+    for dtype in (torch.bfloat16, torch.float16, torch.float32):
+        buf = torch.full((rows + 1, cols + 5), 9.0, dtype=dtype, device="cuda")
+        out = buf[:rows, 3:cols + 3]
+        q.qgtc_fp8_product(X, W, out=out)
+        device_close(out, want, device_tol(x, w, dtype == torch.float32))
+        buf[:rows, 3:cols + 3] = 9.0
+        assert bool((buf == 9.0).all())
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows,cols,inner", GATED)
+def test_large_gated_and_its_gradients(rows, cols, inner, act):
+    (X, x), (G, wg), (P, wu) = on_device(rows, cols, inner, (1, 2, 3))
+    g, u = x @ wg.t().contiguous(), x @ wu.t().contiguous()
+    for dtype in (torch.bfloat16, torch.float16, torch.float32):
+        tg, tu = device_tol(x, wg, dtype == torch.float32), device_tol(x, wu, dtype == torch.float32)
+        if act == "silu":
+            s, curve = torch.sigmoid(g), 0.5
+            a, slope = g * s, s * (1 + g * (1 - s))
+        else:
+            k = (2 / np.pi) ** 0.5
+            s, curve = torch.sigmoid(2 * k * (g + 0.044715 * g ** 3)), 1.2
+            a, slope = g * s, s + g * s * (1 - s) * 2 * k * (1 + 3 * 0.044715 * g * g)
+        own = 16 * 2.0 ** -24
+        # (the short form of the sigmoid, for results of 16 and 8 bits, is off by |z| 2^-24 of it, z the sigmoid's argument; s |z| is
+        # below |g| + 1 for both, and so is its effect on the slope)
+        ta = 1.13 * tg + own * (a.abs() + 1)
+        ts = curve * tg + own * (1 + slope.abs()) + own * g.abs()
+        h, th = a * u, 1.01 * (ta * u.abs() + a.abs() * tu + ta * tu + 2.0 ** -23 * (a * u).abs())
+        room = torch.full((rows, cols + 3), 9.0, dtype=dtype, device="cuda")
+        m = q.qgtc_fp8_gated(X, G, P, act, h=room[:, 1:cols + 1])
+        device_close(room[:, 1:cols + 1], h, th)
+        assert bool((room[:, 0] == 9.0).all()) and bool((room[:, cols + 1:] == 9.0).all())
+        both = [m]
+        if dtype == torch.bfloat16:
+            both.append(q.qgtc_fp8_gated(X, G, P, act))
+        for m in both:
+            e = m.scales[:, :m.blocks].double()
+            got = m.codes.double() * e.repeat_interleave(128, 1)
+            assert bool((m.codes[:, cols:].view(torch.uint8) == 0).all())
+            half = torch.maximum(h.abs() * 2.0 ** -4, 2.0 ** -10 * e.repeat_interleave(128, 1)[:, :cols])
+            bad = (got[:, :cols] - h).abs() > half + th * 1.0625
+            assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist())
+            top = torch.nn.functional.pad(h.abs(), (0, -cols % 128)).view(rows, -1, 128).amax(2)
+            slack = torch.nn.functional.pad(th, (0, -cols % 128)).view(rows, -1, 128).amax(2)
+            assert bool((448 * e >= top - slack).all()) and bool((224 * e < top + slack).all())
+        dh = torch.randn((rows, cols), device="cuda").to(dtype)
+        d = q.qgtc_fp8_gated_backward(X, G, P, dh, act)
+        f = dh.double()
+        device_close(d[:, :cols], f * slope * u, f.abs() * (ts * u.abs() + slope.abs() * tu + ts * tu) * 1.01 + 2.0 ** -22 * (f * slope * u).abs())
+        device_close(d[:, cols:], f * a, f.abs() * ta * 1.01 + 2.0 ** -22 * (f * a).abs())
+
+
+def test_large_rows_keep_to_themselves():
+    """A row of X with an infinity, in the first and in the last tile: no other row changes, by tiles of either size."""
+    for rows, cols, inner in ((300, 4100, 2050), (4090, 4090, 1100)):
+        xs = U.activations(rows, inner, 1)
+        (G, _), (P, _) = on_device(cols, cols, inner, (2, 3))
+        want, wp = q.qgtc_fp8_gated(q.qgtc_fp8_quantize(xs.cuda()), G, P), q.qgtc_fp8_product(q.qgtc_fp8_quantize(xs.cuda()), G)
+        bad = [0, 17, rows - 1]
+        for r in bad:
+            xs[r, inner - 1] = float("inf")
+        X = q.qgtc_fp8_quantize(xs.cuda())
+        got, gp = q.qgtc_fp8_gated(X, G, P), q.qgtc_fp8_product(X, G)
+        ok = torch.ones(rows, dtype=torch.bool)
+        ok[bad] = False
+        assert (U.raw(got.codes)[ok] == U.raw(want.codes)[ok]).all() and (U.raw(got.scales)[ok][:, :got.blocks] == U.raw(want.scales)[ok][:, :got.blocks]).all()
+        assert torch.equal(gp[ok], wp[ok]) and bool(torch.isnan(gp[bad]).all())
+        assert (U.raw(got.scales)[bad][:, :got.blocks] == 255).all() and (U.raw(got.codes)[bad][:, cols:] == 0).all()
+        assert (U.raw(got.codes)[bad][:, :cols] == 0x7f).all()
+
+
 @pytest.mark.parametrize("rows,cols,inner", [(8, 8192, 512), (512, 8192, 520), (4096, 8192, 512)])
 def test_gated_scales_are_those_of_fp32_sums(rows, cols, inner):
     """Every block's scale, but where the largest entry lies within 2^-18 of a border between two (sums of 512 products in fp32 are off
