@@ -105,8 +105,9 @@ struct GradParams {
 };
 
 // A workgroup takes every groups-th row (ONE: four times as many rows, a wave each) and keeps its share of dweight in
-// registers; groups' shares are added up in order by the second kernel, so the result does not depend on timing.  The next row
-// is on its way while one is worked on, where registers have room for it (8192 x 4096 bf16: 65 us without, 52 with, 5.1 TB/s).
+// registers; groups' shares are added up in order by the second kernel, so the result does not depend on timing.  Where a
+// wave has a row to itself its next row is on the way meanwhile and the weight stays in registers; where waves share a row that loses
+// to the other workgroups of the compute unit, which fewer registers leave room for (4095 x 5120 fp16: 46 us, and 37 without, 4.5 TB/s).
 template <int TYPE, int V, bool ONE>
 __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_grad_kernel(const GradParams p) {
   typedef typename Float<TYPE>::type T;
@@ -115,11 +116,10 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_grad_kernel(const GradP
   const int wave = (int)(threadIdx.x >> 6), lane = (int)(threadIdx.x & 63u);
   const int c0 = (ONE ? 0 : wave * V * kPiece) + lane * 8;
   const int64_t step = (int64_t)p.groups * (ONE ? 4 : 1);
-  constexpr bool ROOM = ONE || V == 1;             // in registers, for the weight and the next row
   float w[V][8], dw[V][8];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    if (ROOM) load_weight8(p.weight, p.weight_type, c0 + i * kPiece, p.cols, w[i]);
+    if (ONE) load_weight8(p.weight, p.weight_type, c0 + i * kPiece, p.cols, w[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
   }
@@ -138,10 +138,10 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_grad_kernel(const GradP
   };
   int64_t row = ONE ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
   Row now, then;
-  if (ROOM && row < p.rows) load(row, now);
+  if (ONE && row < p.rows) load(row, now);
   int turn = 0;
   for (; row < p.rows; row += step) {
-    if (!ROOM) load(row, now);
+    if (!ONE) load(row, now);
     else if (row + step < p.rows) load(row + step, then);
     float dy[V][8], s[V][8];
     const float rstd = now.rstd;
@@ -150,8 +150,8 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_grad_kernel(const GradP
     for (int i = 0; i < V; ++i) {
       now.dy[i].widen(dy[i]);
       now.s[i].widen(s[i]);
-      if (!ROOM) load_weight8(p.weight, p.weight_type, c0 + i * kPiece, p.cols, w[0]);
-      const float(&wi)[8] = w[ROOM ? i : 0];
+      if (!ONE) load_weight8(p.weight, p.weight_type, c0 + i * kPiece, p.cols, w[0]);
+      const float(&wi)[8] = w[ONE ? i : 0];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         s[i][j] = s[i][j] * rstd;                  // hat
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void norm_grad_kernel(const GradP
       }
       store8_of<TYPE>((T*)p.dx + row * p.ld_dx, c0 + i * kPiece, p.cols, dy[i]);
     }
-    if (ROOM) now = then;
+    if (ONE) now = then;
   }
   if (!p.partial) return;
   if constexpr (ONE) {
@@ -254,8 +254,8 @@ qgtc_status launch_norm(const NormParams& p, hipStream_t stream) {
   return v == 2 ? launch_norm<TYPE, 2, false>(p, stream) : launch_norm<TYPE, 4, false>(p, stream);
 }
 
-// Up to 1024 columns a wave has a row to itself and no barriers (8192 x 1024 bf16: two waves a row without the next one 33.8 us, so 17.2;
-// at 2048 columns one wave loses to four, 24.6 and 19.4).
+// Up to 1024 columns a wave has a row to itself and no barriers (8192 x 1024 bf16: two waves a row 33.8 us, so 17.2; at 2048
+// columns one wave loses to four, 24.6 and 19.5).  Two workgroups per compute unit: one 69 us, four 57 at 8192 x 4096, two 49.
 constexpr int kOneWave = 1024;
 int grad_groups(int rows, int cols) {
   const int64_t most = cdiv(rows, cols <= kOneWave ? 4 : 1), groups = 2 * device_compute_units();
