@@ -217,8 +217,7 @@ def lib():
         "qgtc_rms_norm": (C.c_int, [P(_NormC), vp]),
         "qgtc_rms_norm_backward_workspace_bytes": (sz, [i32, i32]),
         "qgtc_rms_norm_backward": (C.c_int, [P(_NormGradC), vp, sz, vp]),
-        "qgtc_fp8_product_workspace_bytes": (sz, [i32, i32, i32]),
-        "qgtc_fp8_product": (C.c_int, [P(_Fp8C), P(_Fp8C), i32, vp, i64, vp, sz, vp]),
+        "qgtc_fp8_product": (C.c_int, [P(_Fp8C), P(_Fp8C), i32, vp, i64, vp]),
         "qgtc_fp8_gated_workspace_bytes": (sz, [i32, i32, i32]),
         "qgtc_fp8_gated": (C.c_int, [P(_Fp8C), P(_Fp8C), P(_Fp8C), i32, P(_Fp8C), i32, vp, i64, vp, sz, vp]),
         "qgtc_fp8_gated_backward": (C.c_int, [P(_Fp8C), P(_Fp8C), P(_Fp8C), i32, i32, vp, i64, vp, i64, vp, i64, vp]),

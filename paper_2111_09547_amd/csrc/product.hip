@@ -228,19 +228,11 @@ qgtc_status check_operands(const qgtc_fp8* X, const qgtc_fp8* W, const qgtc_fp8*
 }  // namespace
 }  // namespace qgtc
 
-extern "C" size_t qgtc_fp8_product_workspace_bytes(int32_t rows, int32_t cols, int32_t inner) {
-  (void)rows; (void)cols; (void)inner;
-  return 0;
-}
-
-extern "C" qgtc_status qgtc_fp8_product(const qgtc_fp8* X, const qgtc_fp8* W, int32_t type, void* out, int64_t ld_out,
-                                        void* workspace, size_t workspace_bytes, void* stream) {
+extern "C" qgtc_status qgtc_fp8_product(const qgtc_fp8* X, const qgtc_fp8* W, int32_t type, void* out, int64_t ld_out, void* stream) {
   using namespace qgtc;
-  (void)workspace_bytes;
   qgtc_status st = check_operands(X, W, nullptr);
   if (st != QGTC_OK) return st;
   if (!float_type(type)) return QGTC_ERR_UNSUPPORTED;
-  if (((uintptr_t)workspace & 15u) != 0) return QGTC_ERR_ALIGN;
   if (X->rows == 0 || W->rows == 0) return QGTC_OK;
   if ((st = check_matrix(out, type, X->rows, W->rows, ld_out)) != QGTC_OK) return st;
   ProductParams p{};

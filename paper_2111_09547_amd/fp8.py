@@ -45,6 +45,14 @@ def _run(fn, device: int, *args):
         raise B.QgtcError(status, fn.__name__)
 
 
+def _bytes(fn, device: int, *args) -> int:
+    """A workspace's size, which goes by the device it is asked on."""
+    if device == _device_now():
+        return fn(*args)
+    with torch.cuda.device(device):
+        return fn(*args)
+
+
 def _matrix(t: torch.Tensor, what: str, device: int | None = None, shape=None, dtype=None) -> int:
     """Checks a row-major device matrix; its leading dimension."""
     size, step = t.shape, t.stride()
@@ -192,7 +200,7 @@ def qgtc_rms_norm_backward(dy: torch.Tensor, sum: torch.Tensor, weight: torch.Te
     if dweight:
         dw = _empty(cols, dtype=torch.float32, device=sum.device)
         n.dweight = dw.data_ptr()
-        nbytes = _L.qgtc_rms_norm_backward_workspace_bytes(rows, cols)
+        nbytes = _bytes(_L.qgtc_rms_norm_backward_workspace_bytes, device, rows, cols)
         ws = _empty(nbytes, dtype=torch.uint8, device=sum.device)
     _run(_L.qgtc_rms_norm_backward, device, _byref(n), ws.data_ptr() if nbytes else None, nbytes)
     return dx, dw
@@ -208,16 +216,13 @@ def _same_device(x: Fp8, *others: Fp8) -> int:
 def qgtc_fp8_product(x: Fp8, w: Fp8, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """x.w' (a row of w per output column), sums in fp32."""
     device = _same_device(x, w)
-    shape = (x.c.rows, w.c.rows)
+    shape = (x.rows, w.rows)
     if out is None:
         if dtype not in _TYPES:
             raise TypeError(f"float32, float16 or bfloat16 is wanted, not {dtype}")
         out = _strided(shape, (shape[1], 1), dtype=dtype, device=x.codes.device)
     ld = _matrix(out, "out", device, shape)
-    nbytes = _L.qgtc_fp8_product_workspace_bytes(shape[0], shape[1], x.c.cols)
-    ws = _empty(nbytes, dtype=torch.uint8, device=x.codes.device) if nbytes else None
-    _run(_L.qgtc_fp8_product, device, _byref(x.c), _byref(w.c), _TYPES[out.dtype], out.data_ptr(), ld,
-         ws.data_ptr() if nbytes else None, nbytes)
+    _run(_L.qgtc_fp8_product, device, _byref(x.c), _byref(w.c), _TYPES[out.dtype], out.data_ptr(), ld)
     return out
 
 
@@ -225,7 +230,7 @@ def qgtc_fp8_gated(x: Fp8, gate: Fp8, up: Fp8, act: str = "silu", out: Fp8 | Non
                    h: torch.Tensor | None = None) -> Fp8 | None:
     """act(x.gate') * (x.up') in 8-bit floats; h: a matrix that takes it in its own type (then fp8=False leaves it at that)."""
     device = _same_device(x, gate, up)
-    rows, cols = x.c.rows, gate.c.rows
+    rows, cols = x.rows, gate.rows
     kind = ptr = ws = None
     ld = nbytes = 0
     if h is not None:
@@ -233,7 +238,7 @@ def qgtc_fp8_gated(x: Fp8, gate: Fp8, up: Fp8, act: str = "silu", out: Fp8 | Non
         kind, ptr = _TYPES[h.dtype], h.data_ptr()
     if fp8 or out is not None:
         out = _result(out, rows, cols, x.codes)
-        nbytes = _L.qgtc_fp8_gated_workspace_bytes(rows, cols, x.c.cols)
+        nbytes = _bytes(_L.qgtc_fp8_gated_workspace_bytes, device, rows, cols, x.cols)
         ws = _empty(nbytes, dtype=torch.uint8, device=x.codes.device) if nbytes else None
     _run(_L.qgtc_fp8_gated, device, _byref(x.c), _byref(gate.c), _byref(up.c), _ACTS[act],
          _byref(out.c) if out is not None else None, kind or 0, ptr, ld, ws.data_ptr() if nbytes else None, nbytes)
@@ -244,7 +249,7 @@ def qgtc_fp8_gated_backward(x: Fp8, gate: Fp8, up: Fp8, dh: torch.Tensor, act: s
                             out: torch.Tensor | None = None) -> torch.Tensor:
     """The gradients of x.gate' and of x.up' from that of qgtc_fp8_gated's result: one matrix, the first beside the second."""
     device = _same_device(x, gate, up)
-    rows, cols = x.c.rows, gate.c.rows
+    rows, cols = x.rows, gate.rows
     ld_dh = _matrix(dh, "dh", device, (rows, cols))
     if out is None:
         out = _empty((rows, 2 * cols), dtype=dh.dtype, device=dh.device)

@@ -122,13 +122,13 @@ def test_product_refuses(b):
     f = b.lib().qgtc_fp8_product
     X, W = form(b, 8, 300), form(b, 20, 300)
 
-    def call(x=X, w=W, type=0, out=0x30000, ld=20, ws=None, nbytes=0):
-        return f(C.byref(x) if x else None, C.byref(w) if w else None, type, out, ld, ws, nbytes, None)
+    def call(x=X, w=W, type=0, out=0x30000, ld=20):
+        return f(C.byref(x) if x else None, C.byref(w) if w else None, type, out, ld, None)
     assert call(x=None) == NULL and call(w=None) == NULL and call(out=None) == NULL
     assert call(x=form(b, 8, 300, codes=None)) == NULL
     assert call(w=form(b, 20, 301)) == SHAPE and call(ld=19) == SHAPE and call(x=form(b, 8, 300, ld=256)) == SHAPE
     assert call(type=3) == UNSUPPORTED
-    assert call(out=0x30002) == ALIGN and call(type=2, out=0x30001) == ALIGN and call(ws=0x40004) == ALIGN
+    assert call(out=0x30002) == ALIGN and call(type=2, out=0x30001) == ALIGN
     assert call(x=form(b, 8, 300, ld=448)) == ALIGN and call(w=form(b, 20, 300, codes=0x10004)) == ALIGN
     for more in ({"ld": (1 << 24) + 128}, {"ld_scales": (1 << 24) + 4}):
         assert call(x=form(b, 8, 300, **more)) == UNSUPPORTED and call(w=form(b, 20, 300, **more)) == UNSUPPORTED
