@@ -262,6 +262,23 @@ def test_product_of_extreme_scales():
         U.close(q.qgtc_fp8_product(X, W, dtype), want, U.product_tol(x, w, dtype == torch.float32) * 1.01 + U.rounded_tol(want, dtype))
 
 
+@pytest.mark.parametrize("rows", [5, 300])
+def test_product_of_the_smallest_scales(rows):
+    """Blocks whose scale is 2^-127 and a little more."""
+    xs, ws = U.activations(rows, 384, 1), U.weights(300, 384, 2) * 2.0 ** 100
+    xs[:, :128] *= 2.0 ** -126
+    xs[:, 128:256] *= 2.0 ** -122
+    xs[:, 256:] *= 2.0 ** -118
+    (X, x), (W, w) = fp8_of(xs), fp8_of(ws)
+    assert (U.raw(X.scales)[:, 0] == 0).all() and (U.raw(X.scales)[:, 2] > 0).any()
+    want = x @ w.T
+    for dtype in (torch.bfloat16, torch.float32):
+        tol = U.product_tol(x, w, dtype == torch.float32) * 1.01 + U.rounded_tol(want, dtype)
+        if dtype == torch.float32:                      # values below 2^-126 go as subnormal bf16, with steps of 2^-133
+            tol = tol + 2.0 ** -134 * np.abs(w).sum(1)[None, :]
+        U.close(q.qgtc_fp8_product(X, W, dtype), want, tol, dtype)
+
+
 def test_product_of_nothing():
     X, W = q.Fp8(torch.empty((5, 0), dtype=torch.uint8, device="cuda"), torch.empty((5, 0), dtype=torch.uint8, device="cuda")), \
         q.Fp8(torch.empty((300, 0), dtype=torch.uint8, device="cuda"), torch.empty((300, 0), dtype=torch.uint8, device="cuda"))
