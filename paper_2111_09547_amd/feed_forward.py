@@ -11,6 +11,13 @@ import torch
 from . import fp8 as F
 
 
+def _packed(w: torch.Tensor, old: F.Fp8 | None, columns: bool = False) -> F.Fp8:
+    rows, cols = reversed(w.shape) if columns else w.shape
+    if old is not None and (old.rows, old.cols, old.device) != (rows, cols, w.get_device()):
+        old = None
+    return F.qgtc_fp8_quantize(w, columns=columns, out=old)
+
+
 class GatedFeedForward:
     """norm_weight [D], gate and up [H, D], down [D, H]: float32, float16 or bfloat16 on one device, quantized once by pack().
     training: forward() keeps its intermediate results until backward()."""
@@ -22,15 +29,18 @@ class GatedFeedForward:
         self.norm_weight, self.gate, self.up, self.down = norm_weight, gate, up, down
         self.eps, self.act, self.training = eps, act, training
         self._kept = None
+        self.gate_q = self.up_q = self.down_q = self.down_t = self.gate_up_t = None
         self.pack()
 
     def pack(self):
         """Weights into 8-bit floats; to be called again when any of them has changed.  For training also along the other axis,
-        as the backward pass contracts over it."""
-        self.gate_q, self.up_q, self.down_q = (F.qgtc_fp8_quantize(w) for w in (self.gate, self.up, self.down))
+        as the backward pass contracts over it.  Weights of the sizes and the device of before go where those were, since a
+        recorded pass reads them there: passes on other streams have to be done with them."""
+        self.gate_q, self.up_q = _packed(self.gate, self.gate_q), _packed(self.up, self.up_q)
+        self.down_q = _packed(self.down, self.down_q)
         if self.training:
-            self.down_t = F.qgtc_fp8_quantize(self.down, columns=True)
-            self.gate_up_t = F.qgtc_fp8_quantize(torch.cat([self.gate, self.up]), columns=True)
+            self.down_t = _packed(self.down, self.down_t, columns=True)
+            self.gate_up_t = _packed(torch.cat([self.gate, self.up]), self.gate_up_t, columns=True)
 
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
         """(y, s) of x [T, D]: the block's result, which the next norm adds to s."""

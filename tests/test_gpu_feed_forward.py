@@ -175,3 +175,27 @@ def test_refuses():
         q.qgtc_fp8_product(q.alloc_fp8(4, 256, "cuda"), q.alloc_fp8(4, 300, "cuda"))
     with pytest.raises(KeyError):
         q.qgtc_fp8_gated(q.alloc_fp8(4, 256, "cuda"), b.gate_q, b.up_q, "tanh")
+
+
+def test_recorded_pass_takes_weights_packed_again():
+    """pack() leaves the weights where a recorded pass reads them; those of other sizes go elsewhere."""
+    b = block(256, 300, torch.bfloat16, "silu", training=True)
+    b.training = False
+    x = U.activations(20, 256, 1).bfloat16().cuda()
+    graph, y, _ = b.capture(x)
+    before = [m.codes.data_ptr() for m in (b.gate_q, b.up_q, b.down_q)]
+    for k in range(3):
+        b.gate.copy_(U.weights(300, 256, 20 + k))
+        b.down = U.weights(256, 300, 30 + k).bfloat16().cuda()
+        b.pack()
+        assert [m.codes.data_ptr() for m in (b.gate_q, b.up_q, b.down_q)] == before
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, b.forward(x)[0])
+    held = b.gate_q
+    b.gate, b.up = (U.weights(100, 256, k).bfloat16().cuda() for k in (40, 41))
+    b.down = U.weights(256, 100, 42).bfloat16().cuda()
+    b.pack()
+    assert (b.gate_q.rows, b.down_q.cols) == (100, 100) and held.codes.data_ptr() == before[0]
+    fresh = GatedFeedForward(b.norm_weight, b.gate, b.up, b.down)
+    assert torch.equal(b.forward(x)[0], fresh.forward(x)[0])
