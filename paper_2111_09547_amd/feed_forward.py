@@ -67,7 +67,8 @@ class GatedFeedForward:
         return {"x": dx, "norm_weight": dw, "gate": gate_up[:hidden], "up": gate_up[hidden:], "down": down}
 
     def capture(self, x: torch.Tensor, residual: torch.Tensor | None = None):
-        """(graph, y, s): one forward pass on these tensors as a HIP graph; a replay reads what x and residual hold then."""
+        """(graph, y, s): one forward pass on these tensors as a HIP graph; a replay reads what x and residual hold then.
+        The graph keeps what it reads."""
         if self.training:
             raise RuntimeError("a block that is training is not recorded")
         stream = torch.cuda.Stream(x.device)
@@ -78,4 +79,5 @@ class GatedFeedForward:
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             y, s = self.forward(x, residual)
+        graph.reads = (x, residual, self.norm_weight, self.gate_q, self.up_q, self.down_q)
         return graph, y, s

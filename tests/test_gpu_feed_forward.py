@@ -199,3 +199,19 @@ def test_recorded_pass_takes_weights_packed_again():
     assert (b.gate_q.rows, b.down_q.cols) == (100, 100) and held.codes.data_ptr() == before[0]
     fresh = GatedFeedForward(b.norm_weight, b.gate, b.up, b.down)
     assert torch.equal(b.forward(x)[0], fresh.forward(x)[0])
+
+
+def test_recorded_pass_keeps_what_it_reads():
+    """The block and its inputs are let go, and the memory that this frees is written."""
+    b = block(384, 500, torch.bfloat16, "gelu")
+    x, res = (U.activations(40, 384, k).bfloat16().cuda() for k in (1, 2))
+    graph, y, s = b.capture(x, res)
+    want = [t.clone() for t in b.forward(x, res)]
+    sizes = [t.numel() * t.element_size() for t in (x, res, b.norm_weight, b.gate_q.codes, b.gate_q.scales, b.down_q.codes, b.down_q.scales)]
+    del b, x, res
+    for _ in range(3):
+        taken = [torch.full((n,), 0x55, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(s, want[1])
+        del taken
