@@ -76,8 +76,9 @@ class GatedFeedForward:
         with torch.cuda.stream(stream):                  # what is done once per kernel is done outside the recording
             self.forward(x, residual)
         torch.cuda.current_stream(x.device).wait_stream(stream)
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
-            y, s = self.forward(x, residual)
+        with torch.cuda.device(x.device):                # (a recording is on the current device's stream otherwise)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                y, s = self.forward(x, residual)
         graph.reads = (x, residual, self.norm_weight, self.gate_q, self.up_q, self.down_q)
         return graph, y, s

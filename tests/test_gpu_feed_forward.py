@@ -215,3 +215,22 @@ def test_recorded_pass_keeps_what_it_reads():
         torch.cuda.synchronize()
         assert torch.equal(y, want[0]) and torch.equal(s, want[1])
         del taken
+
+
+def test_recorded_on_the_device_of_its_inputs(monkeypatch):
+    """On a stream of that device, whichever is current."""
+    index = torch.cuda.device_count() - 1
+    b = block(256, 300, torch.bfloat16, "silu")
+    for name in ("norm_weight", "gate", "up", "down"):
+        setattr(b, name, getattr(b, name).to(f"cuda:{index}"))
+    b.pack()
+    x = U.activations(20, 256, 1).bfloat16().to(f"cuda:{index}")
+    streams, graph_of = [], torch.cuda.graph
+    monkeypatch.setattr(torch.cuda, "graph", lambda graph, stream=None: (streams.append(stream), graph_of(graph, stream=stream))[1])
+    with torch.cuda.device(0):
+        graph, y, _ = b.capture(x)
+        assert torch.cuda.current_device() == 0
+        graph.replay()
+    assert streams[0] is not None and streams[0].device.index == index == y.get_device()
+    torch.cuda.synchronize(index)
+    assert torch.equal(y, b.forward(x)[0])
