@@ -710,7 +710,8 @@ qgtc_status qgtc_fold_batchnorm(const double* gamma, const double* beta, const d
  * A matrix has at most 2^29 rows and columns (QGTC_ERR_SHAPE).
  *
  * Other tensors are row-major in one of three types, with a leading dimension in elements
- * (any that is at least the number of columns) and the alignment of their type.
+ * (any that is at least the number of columns) and the alignment of their type.  Outputs
+ * and workspaces overlap neither inputs nor each other, but where a call says otherwise.
  * ------------------------------------------------------------------------- */
 enum { QGTC_F32 = 0, QGTC_F16 = 1, QGTC_BF16 = 2 };
 
