@@ -128,6 +128,12 @@ __device__ __forceinline__ bool near_border(uint32_t top) {
 }
 // The bits from which on an entry may be the largest of such a block.
 __device__ __forceinline__ uint32_t border_from(uint32_t top) { return ((top & 0x7f800000u) | 0x600000u) - kNear; }
+// What such a block's scale is made from: the border itself or the next number above it, by the entry that was computed again, and nothing
+// further away.  Where sums cancel that entry may be any number, but the codes are of the sums that were cut, with `top` among them.
+__device__ __forceinline__ uint32_t border_side(uint32_t top, uint32_t exact) {
+  const uint32_t border = (top & 0x7f800000u) | 0x600000u;
+  return exact > border ? border + 1u : border;
+}
 
 // h of row m and column n (of all lanes alike), by all 64 lanes: 16 codes a lane at a time.
 __device__ __forceinline__ float exact_h(const ProductParams& p, int64_t m, int64_t n) {

@@ -168,7 +168,7 @@ __global__ __launch_bounds__(256) void gated_rows_kernel(const ProductParams p, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) want |= near && abs_bits(v[i]) >= border_from(top) ? 1u << i : 0u;
     const uint32_t block = max_of_16_lanes(exact_top(p, m, c, want));
-    if (near) top = block;
+    if (near) top = border_side(top, block);
   }
   write_block8(p.codes + (int64_t)m * p.ld_codes, p.scales + (int64_t)m * p.ld_scales, c, p.cols, v, scale_byte(top));
 }

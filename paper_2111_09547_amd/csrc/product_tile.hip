@@ -237,7 +237,8 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
           uint32_t exact = exact_top(p, m0 + lr, n0, mine);
           exact = max(exact, (uint32_t)__shfl_xor((int)exact, 16));
           exact = max(exact, (uint32_t)__shfl_xor((int)exact, 32));
-          if (g == 0 && near_border(max(tops[lr], tops[kTile + lr]))) again[wn * kTile + lr] = exact;
+          const uint32_t top = max(tops[lr], tops[kTile + lr]);
+          if (g == 0 && near_border(top)) again[wn * kTile + lr] = border_side(top, exact);
         }
       }
       meet_lds();
