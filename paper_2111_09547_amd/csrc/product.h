@@ -87,16 +87,17 @@ __device__ __forceinline__ v8i lane_codes(const uint8_t* p) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// exp(-z) with one more step than the instruction alone: the product with log2(e) is rounded, and what the rounding left off is put
-// back, so that the relative error stays near one unit for every z instead of growing with it.  |z| is held to 87, beyond which
-// the sigmoid is 1 or below 2^-125.
-__device__ __forceinline__ float exp_minus(float z) {
-  z = __builtin_amdgcn_fmed3f(z, -87.0f, 87.0f);
-  const float hi = z * -1.44269504f, lo = fmaf(z, -1.44269504f, -hi) + z * -1.92596299e-8f;
+// exp(-a) for a >= 0 with one more step than the instruction alone: the product with log2(e) is rounded, and what the rounding left off
+// is put back, so that the relative error stays near one unit for every a instead of growing with it.  0 where it is below 2^-126.
+__device__ __forceinline__ float exp_minus(float a) {
+  a = a > 150.0f ? 150.0f : a;                       // (an infinity times its rounding is NaN; NaN stays)
+  const float hi = a * -1.44269504f, lo = fmaf(a, -1.44269504f, -hi) + a * -1.92596299e-8f;
   const float e = __builtin_amdgcn_exp2f(hi);
   return fmaf(e, lo * 0.693147181f, e);
 }
 // act(g) = g * s(z(g)), s the sigmoid, z = g (silu) or 2 sqrt(2/pi) (g + 0.044715 g^3) (gelu: (1 + tanh(z/2)) / 2 = s(z)).
+// Its slope is s + g z' s (1 - s).  g z' grows as g^3 and beyond fp32's range, while s (1 - s) is 0 from |z| = 88 on, where g z' is below
+// 3 * 88: held to 512 it changes no product that is not 0 anyway, and no infinity meets a 0.
 struct Gate {
   float value, slope;
 };
@@ -108,13 +109,15 @@ __device__ __forceinline__ Gate gate(int act, float g) {
     z = k * fmaf(0.044715f * g2, g, g);
     dz = k * fmaf(0.134145f, g2, 1.0f);
   }
+  const float t = __builtin_amdgcn_fmed3f(g * dz, -512.0f, 512.0f);   // (of NaN anything: s is NaN then)
   if constexpr (PRECISE) {
-    const float e = exp_minus(z), s = __builtin_amdgcn_rcpf(1.0f + e);
-    return {g * s, s * fmaf(g * dz, e * s, 1.0f)};     // 1 - s = e s
+    const float e = exp_minus(fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + e), less = e * r;   // the sigmoids of |z| and -|z|
+    const float s = z < 0.0f ? less : r;
+    return {g * s, fmaf(t, less * r, s)};
   } else {
     // For results of 16 and 8 bits: off by |z| 2^-24 of the sigmoid, which is below 2^-16 where it is not below 2^-360 itself.
     const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
-    return {g * s, s * fmaf(g * dz, 1.0f - s, 1.0f)};
+    return {g * s, s * fmaf(t, 1.0f - s, 1.0f)};
   }
 }
 

@@ -38,3 +38,56 @@ def test_gated_scale_where_sums_cancel(rows, cols, inner, groups, small):
     lo, hi = 8 * min(56.0, max(exact, -0.3)), 8 * max(56.0, exact)
     assert bool((got[:, 1:] == 416.0).all())                     # (13 * 32: an e4m3)
     assert bool((got[:, 0] >= lo * (1 + 2.0 ** -4 * np.sign(-lo))).all() and (got[:, 0] <= hi * (1 + 2.0 ** -4)).all()), got[:2, 0].tolist()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows,cols,inner", [(40, 128, 256)] + SIZES[1:])
+def test_gates_to_the_end_of_their_range(rows, cols, inner, act):
+    """Every gate is one product, which is exact, and u is 1: h, dg and du are the activation, its slope and itself.
+
+    Bounds: the sigmoid is 88 * 2^-24 < 2^-17 of itself off at most (the instruction's argument is rounded) and 0 below 2^-126; a few
+    roundings come to less than as much again.  In the slope it is s and g z' s (1 - s) that are off by so much, and where 1 - s is a
+    difference of fp32 (z > 0, to z = 17.4, g z' < 53) that by 2^-24: 53 * 2^-24 < 2^-18."""
+    vals = [s * v for v in (0.25, 1.0, 3.0, 16.0, 80.0, 96.0, 1e3, 1e4, 1e8, 1e12, 5e12, 1e13, 2e13, 1e18, 3e19, 1e25, 1e37, 1.5e38) for s in (1, -1)]
+    x = torch.zeros((rows, inner))
+    x[:len(vals), 0], x[:, 128] = torch.tensor(vals), 1.0
+    one = torch.zeros((2, cols, inner))
+    one[0, :, 0], one[1, :, 128] = 1.0, 1.0
+    X, G, P = (q.qgtc_fp8_quantize(t.cuda()) for t in (x, *one))
+    g = on_device(X)[:, 0].double()
+    if act == "silu":
+        z, gdz = g, g.clone()
+    else:
+        k = 2 * (2 / np.pi) ** 0.5
+        z, gdz = k * (g + 0.044715 * g ** 3), k * (g + 3 * 0.044715 * g ** 3)
+    s = torch.sigmoid(z)
+    bend = torch.where(z.abs() < 700, gdz * s * torch.sigmoid(-z), torch.zeros_like(z))
+    value, slope = (g * s)[:, None], (s + bend)[:, None]
+    off = (g.abs() * (s * 2.0 ** -16 + 2.0 ** -126))[:, None]
+    off_slope = ((s + bend.abs()) * 2.0 ** -16 + (z > 0) * 2.0 ** -18 + 513 * 2.0 ** -126)[:, None]
+
+    def check(got, want, tol):
+        bad = ~((got.double() - want).abs() <= tol + want.abs() * U.HALF[got.dtype] + U.TINY[got.dtype])
+        assert not bool(bad.any()), (got.dtype, [(g[i].item(), got[i, j].item(), want[i, 0].item()) for i, j in bad.nonzero()[:4].tolist()])
+    for dtype in (torch.float32, torch.bfloat16):
+        h = torch.empty((rows, cols), dtype=dtype, device="cuda")
+        m = q.qgtc_fp8_gated(X, G, P, act, h=h)
+        check(h, value, off)
+        assert not bool((m.scales.view(torch.uint8)[:, :m.blocks] == 255).any())
+        d = q.qgtc_fp8_gated_backward(X, G, P, torch.ones((rows, cols), dtype=dtype, device="cuda"), act)
+        check(d[:, :cols], slope, off_slope)
+        check(d[:, cols:], value, off)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows,cols,inner", [(40, 128, 256)] + SIZES[1:])
+def test_gates_of_nan(rows, cols, inner, act):
+    """A NaN in a gate is one in the value and in the slope."""
+    x = torch.zeros((rows, inner))
+    x[3, 0], x[:, 128] = float("nan"), 1.0
+    one = torch.zeros((2, cols, inner))
+    one[0, :, 0], one[1, :, 128] = 1.0, 1.0
+    X, G, P = (q.qgtc_fp8_quantize(t.cuda()) for t in (x, *one))
+    for dtype in (torch.float32, torch.bfloat16):
+        d = q.qgtc_fp8_gated_backward(X, G, P, torch.ones((rows, cols), dtype=dtype, device="cuda"), act)
+        assert bool(d[3].isnan().all()) and not bool(d[:3].isnan().any()) and not bool(d[4:].isnan().any())
