@@ -16,19 +16,22 @@ __global__ __launch_bounds__(512) void few_kernel(const ProductParams p) {
   const int r = lane & 15, g = lane >> 4;
   const int n0 = (int)blockIdx.x * 16, m0 = (int)blockIdx.y * (16 * MT);
   const uint8_t *wc[D], *ws[D], *xc[MT], *xs[MT];
+  auto aim = [&](int r) {
 #pragma unroll
-  for (int d = 0; d < D; ++d) {
-    const Fp8Operand& w = d ? p.u : p.w;
-    const int64_t n = min(n0 + r, p.cols - 1);
-    wc[d] = w.codes + n * w.ld + 16 * g;
-    ws[d] = w.scales + n * w.ld_scales;
-  }
+    for (int d = 0; d < D; ++d) {
+      const Fp8Operand& w = d ? p.u : p.w;
+      const int64_t n = min(n0 + r, p.cols - 1);
+      wc[d] = w.codes + n * w.ld + 16 * g;
+      ws[d] = w.scales + n * w.ld_scales;
+    }
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int64_t m = min(m0 + 16 * t + r, p.rows - 1);
-    xc[t] = p.x.codes + m * p.x.ld + 16 * g;
-    xs[t] = p.x.scales + m * p.x.ld_scales;
-  }
+    for (int t = 0; t < MT; ++t) {
+      const int64_t m = min(m0 + 16 * t + r, p.rows - 1);
+      xc[t] = p.x.codes + m * p.x.ld + 16 * g;
+      xs[t] = p.x.scales + m * p.x.ld_scales;
+    }
+  };
+  aim(r);
   v4f acc[D][MT];
 #pragma unroll
   for (int d = 0; d < D; ++d)
@@ -51,10 +54,10 @@ __global__ __launch_bounds__(512) void few_kernel(const ProductParams p) {
       if constexpr (WIDE) {
         WideCodes wide[MT];
 #pragma unroll
-        for (int t = 0; t < MT; ++t) wide[t] = widen<B>(x[t], sx[t]);
+        for (int t = 0; t < MT; ++t) wide[t] = widen<B, false>(x[t], sx[t]);
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-          const WideCodes v = widen<B>(w[d], sw[d]);
+          const WideCodes v = widen<B, false>(w[d], sw[d]);
 #pragma unroll
           for (int t = 0; t < MT; ++t) acc[d][t] = wide_mfma(v, wide[t], acc[d][t]);
         }
@@ -74,6 +77,43 @@ __global__ __launch_bounds__(512) void few_kernel(const ProductParams p) {
       one(std::integral_constant<int, 0>());
       if (b0 + 1 < p.blocks) one(std::integral_constant<int, 1>());
       if (b0 + 2 < p.blocks) one(std::integral_constant<int, 2>());
+    }
+  }
+  if constexpr (WIDE) {
+    bool none = false;
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) none |= put_back(acc[d][t]);
+    if (__ballot(none)) {                              // this wave's blocks again, one at a time
+      int again = r;
+      asm volatile("" : "+v"(again));                  // (addresses that are kept for this cost the loop above its registers)
+      aim(again);
+#pragma unroll
+      for (int d = 0; d < D; ++d)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[d][t] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+      for (int b = wave * 4; b < p.blocks; b += (b & 3) == 3 ? waves * 4 - 3 : 1) {
+        const int64_t at = (int64_t)b * kBlock;
+        WideCodes x[MT];
+        uint32_t sx[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          sx[t] = xs[t][b];
+          x[t] = widen<0, true>(lane_codes(xc[t] + at), sx[t]);
+        }
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+          const uint32_t sw = ws[d][b];
+          const WideCodes w = widen<0, true>(lane_codes(wc[d] + at), sw);
+          v4i rows;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) rows[i] = __shfl((int)sw, 4 * g + i);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) acc[d][t] = apart_mfma(w, x[t], acc[d][t], rows, 0, sx[t]);
+        }
+      }
     }
   }
 #pragma unroll

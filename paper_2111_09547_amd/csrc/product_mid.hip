@@ -14,7 +14,7 @@ namespace {
 constexpr int kSide = 128;
 constexpr int kOperand = kSide * kBlock, kBuffer = 2 * kOperand;
 constexpr int kScales = 4 * kBuffer, kSlot = 2 * kSide * 4;      // words of four blocks' scales: [2 slots][X, W][128]
-constexpr int kMidLds = kScales + 2 * kSlot;
+constexpr int kFlags = kScales + 2 * kSlot, kMidLds = kFlags + 16;    // a word for each wave
 
 struct MidParams {
   ProductParams p;
@@ -91,53 +91,71 @@ __global__ __launch_bounds__(256, 1) void mid_kernel(const MidParams mp) {
     }
   };
   v4f acc[4][4];                                     // [w][x]
+  auto sums = [&](auto way) {
+    constexpr bool APART = decltype(way)::value;
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int u = 0; u < 4; ++u) acc[t][u] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+      for (int u = 0; u < 4; ++u) acc[t][u] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
 
-  Block b0, b1;
-  load_scales(0);
+    Block b0, b1;
+    load_scales(0);
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) load(k, j);
-  meet<24>();
+      for (int j = 0; j < 4; ++j) load(k, j);
+    meet<24>();
 #pragma unroll
-  for (int t = 0; t < 4; ++t) read(0, b0, t);
-  // 16 products of a block, a quarter of the next one's operands and of the loads in front of every four.  (All of them in front of the
-  // products, products wait until the LDS has taken the reads: a block 0.59 us; in the compiler's order 0.74.)
-  auto step = [&](int k, const Block& now, Block& then) {
-    meet<16>();                                      // block k + 1 has come; everyone has read block k
-    if ((k & 3) == 0) load_scales(k + 4);
-    __builtin_amdgcn_sched_barrier(0);
-    WideCodes x[4];
-    if constexpr (WIDE) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) x[u] = widen<0>(now.x[u], now.sx[u]);
-    }
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      read(k + 1, then, t);                          // (behind the last block: of what is there, not used)
-      load(k + 4, t);
-      if constexpr (WIDE) {
-        const WideCodes w = widen<0>(now.w[t], now.sw[t]);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) acc[t][u] = wide_mfma(w, x[u], acc[t][u]);
-      } else {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) acc[t][u] = block_mfma<0>(now.w[t], now.x[u], acc[t][u], now.sw[t], now.sx[u]);
-      }
+    for (int t = 0; t < 4; ++t) read(0, b0, t);
+    // 16 products of a block, a quarter of the next one's operands and of the loads in front of every four.  (All of them in front of the
+    // products, products wait until the LDS has taken the reads: a block 0.59 us; in the compiler's order 0.74.)
+    auto step = [&](int k, const Block& now, Block& then) {
+      meet<16>();                                    // block k + 1 has come; everyone has read block k
+      if ((k & 3) == 0) load_scales(k + 4);
       __builtin_amdgcn_sched_barrier(0);
-    }
-  };
+      WideCodes x[4];
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = widen<0, APART>(now.x[u], now.sx[u]);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        read(k + 1, then, t);                        // (behind the last block: of what is there, not used)
+        load(k + 4, t);
+        if constexpr (WIDE) {
+          const WideCodes w = widen<0, APART>(now.w[t], now.sw[t]);
+          v4i rows;
+          if constexpr (APART) rows = *reinterpret_cast<const v4i*>(lds + (kScales + (k >> 2 & 1) * kSlot + (kSide + wn * 64 + t * 16 + 4 * g) * 4));
+#pragma unroll
+          for (int u = 0; u < 4; ++u) acc[t][u] = APART ? apart_mfma(w, x[u], acc[t][u], rows, 8 * (k & 3), now.sx[u]) : wide_mfma(w, x[u], acc[t][u]);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) acc[t][u] = block_mfma<0>(now.w[t], now.x[u], acc[t][u], now.sw[t], now.sx[u]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
 #pragma unroll 1
-  for (int k = 0; k + 1 < p.blocks; k += 2) {
-    step(k, b0, b1);
-    step(k + 1, b1, b0);
+    for (int k = 0; k + 1 < p.blocks; k += 2) {
+      step(k, b0, b1);
+      step(k + 1, b1, b0);
+    }
+    if (p.blocks & 1) step(p.blocks - 1, b0, b1);
+    meet<0>();                                       // (nothing is on its way to LDS any more)
+  };
+  sums(std::false_type());
+  if constexpr (WIDE) {                              // (waves share their loads, so all of them again or none)
+    bool none = false;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) none |= put_back(acc[t][u]);
+    uint32_t* const flags = reinterpret_cast<uint32_t*>(lds + kFlags);
+    const uint32_t mine = __ballot(none) != 0ull;
+    if (lane == 0) flags[wave] = mine;
+    meet_lds();
+    if (scalar(flags[0] | flags[1] | flags[2] | flags[3])) sums(std::true_type());
   }
-  if (p.blocks & 1) step(p.blocks - 1, b0, b1);
-  meet<0>();                                         // (nothing is on its way to LDS any more)
 
   // ---- what is made of the sums ----
 #pragma unroll

@@ -91,3 +91,83 @@ def test_gates_of_nan(rows, cols, inner, act):
     for dtype in (torch.float32, torch.bfloat16):
         d = q.qgtc_fp8_gated_backward(X, G, P, torch.ones((rows, cols), dtype=dtype, device="cuda"), act)
         assert bool(d[3].isnan().all()) and not bool(d[:3].isnan().any()) and not bool(d[4:].isnan().any())
+
+
+# sizes for each kernel of fp32 results (few rows, tiles of 128 x 128) and, the last, of 16 bits
+SCALED = [(5, 40), (50, 40), (1000, 2056), (4090, 4090)]
+
+
+def scaled(rows, cols, blocks, sx, sw, seed):
+    """Operands with given scales (bytes [rows, blocks]) and codes of normal data, and their values in 64 bits."""
+    made = []
+    for n, s, k in ((rows, sx, 1), (cols, sw, 2)):
+        c = torch.randn((n, blocks * 128), generator=torch.Generator().manual_seed(seed + k)) * 8
+        c[:, 1::9] *= 20.0
+        codes = c.clamp(-448.0, 448.0).to(torch.float8_e4m3fn).cuda()        # (what is larger becomes NaN)
+        wide = torch.zeros((n, -(-blocks // 4) * 4), dtype=torch.uint8)
+        wide[:, :blocks] = s
+        two = torch.ldexp(torch.ones((n, blocks), dtype=torch.float64), s.int() - 127).cuda()
+        made.append((q.Fp8(codes, wide.cuda(), blocks * 128), codes.double() * two.repeat_interleave(128, 1)))
+    return made
+
+
+def product_close(got, x, w):
+    want = x @ w.t().contiguous()
+    blocks = x.shape[1] // 128
+    tol = (blocks + 128) * 2.0 ** -23 * (x.abs() @ w.abs().t().contiguous())          # (U.product_tol)
+    if got.dtype != torch.float32:
+        tops = [v.abs().view(v.shape[0], -1, 8).amax(2) for v in (x, w)]
+        tol = tol + 7 * 2.0 ** -13 * (tops[0] @ tops[1].t().contiguous())
+    bad = ~((got.double() - want).abs() <= tol * 1.01 + want.abs() * U.HALF[got.dtype] + U.TINY[got.dtype])
+    assert not bool(bad.any()), (got.dtype, int(bad.sum()), [(got[i, j].item(), want[i, j].item()) for i, j in bad.nonzero()[:3].tolist()])
+
+
+@pytest.mark.parametrize("rows,cols", SCALED)
+def test_product_of_scales_from_end_to_end(rows, cols):
+    """Blocks of every scale there is, 0 to 254, against blocks of the opposite scale: every product is of one size, and no partial sum
+    leaves fp32's range."""
+    blocks = 17
+    base = torch.tensor([0, 254, 1, 9, 10, 11, 235, 236, 237, 245, 246, 247, 253, 64, 127, 190, 128])
+    near = [torch.randint(-3, 4, (n, blocks), generator=torch.Generator().manual_seed(n)) for n in (rows, cols + 7)]
+    sx, sw = (base + near[0]).clamp(0, 254).byte(), (254 - base + near[1][:cols]).clamp(0, 254).byte()
+    (X, x), (W, w) = scaled(rows, cols, blocks, sx, sw, 3)
+    for dtype in (torch.float32, torch.bfloat16):
+        product_close(q.qgtc_fp8_product(X, W, dtype), x, w)
+
+
+@pytest.mark.parametrize("rows,cols", SCALED)
+@pytest.mark.parametrize("up", [105, 90, -105, -125])
+def test_product_results_from_end_to_end(rows, cols, up):
+    """Results of about 2^(up + 16), those near fp32's ends among them.  Below 2^-126 a rounding is by half of 2^-149, of each of the two
+    blocks' sums and of the result."""
+    sx, sw = torch.full((rows, 2), 127 + up // 2, dtype=torch.uint8), torch.full((cols, 2), 127 + (up - up // 2), dtype=torch.uint8)
+    (X, x), (W, w) = scaled(rows, cols, 2, sx, sw, 5)
+    assert bool((x @ w.t().contiguous()).abs().max() < 2.0 ** 127)
+    for dtype in (torch.float32, torch.bfloat16):
+        product_close(q.qgtc_fp8_product(X, W, dtype), x, w)
+
+
+@pytest.mark.parametrize("rows,cols", SCALED)
+def test_product_of_the_largest_number(rows, cols):
+    """fp32's largest number becomes 256 * 2^120; multiplied with 2^-100 that is 2^28, and 0 times it is 0."""
+    x, w = torch.zeros((rows, 300)), torch.zeros((cols, 300))
+    x[:, 3], x[:, 200], w[:, 3], w[0, 3], w[:, 200] = torch.finfo(torch.float32).max, 1.0, 2.0 ** -100, 0.0, 3.0
+    X, W = q.qgtc_fp8_quantize(x.cuda()), q.qgtc_fp8_quantize(w.cuda())
+    for dtype in (torch.float32, torch.bfloat16):
+        y = q.qgtc_fp8_product(X, W, dtype)
+        want = torch.tensor(2.0 ** 28 + 3).to(dtype).cuda()
+        assert bool((y[:, 1:] == want).all()) and bool((y[:, 0] == 3.0).all())
+
+
+@pytest.mark.parametrize("rows,cols", SCALED)
+@pytest.mark.parametrize("code", [0x38, 0x00])
+def test_product_of_blocks_without_a_scale(rows, cols, code):
+    """A scale of 255 is NaN and so is its block, whatever the codes: 1 or 0."""
+    ones = torch.ones((rows, 400)), torch.ones((cols, 400))
+    for side in (0, 1):
+        ops = [q.qgtc_fp8_quantize(t.cuda()) for t in ones]
+        ops[side].codes.view(torch.uint8)[2, 128:256], ops[side].scales.view(torch.uint8)[2, 1] = code, 255
+        for dtype in (torch.float32, torch.bfloat16):
+            y = q.qgtc_fp8_product(*ops, dtype)
+            y = y if side == 0 else y.t()
+            assert bool(y[2].isnan().all()) and bool((y[:2] == 400).all()) and bool((y[3:] == 400).all())
