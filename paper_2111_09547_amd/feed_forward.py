@@ -33,12 +33,13 @@ class GatedFeedForward:
         self.pack()
 
     def pack(self):
-        """Weights into 8-bit floats; to be called again when any of them has changed.  For training also along the other axis,
-        as the backward pass contracts over it.  Weights of the sizes and the device of before go where those were, since a
-        recorded pass reads them there: passes on other streams have to be done with them."""
+        """Weights into 8-bit floats; to be called again when any of them has changed, or when training has been set on a block that
+        was made without.  For training also along the other axis, as the backward pass contracts over it: once a block has those,
+        every call brings them up to date, whether it is training then or not.  Weights of the sizes and the device of before go
+        where those were, since a recorded pass reads them there: passes on other streams have to be done with them."""
         self.gate_q, self.up_q = _packed(self.gate, self.gate_q), _packed(self.up, self.up_q)
         self.down_q = _packed(self.down, self.down_q)
-        if self.training:
+        if self.training or self.down_t is not None:
             self.down_t = _packed(self.down, self.down_t, columns=True)
             self.gate_up_t = _packed(torch.cat([self.gate, self.up]), self.gate_up_t, columns=True)
 
@@ -56,6 +57,8 @@ class GatedFeedForward:
         and of the weights ("norm_weight", "gate", "up", "down": float32).  Quantization counts as the identity."""
         if self._kept is None:
             raise RuntimeError("backward() follows a forward() of a block that is training")
+        if self.down_t is None:
+            raise RuntimeError("the block was packed for forward passes alone: pack() once more")
         (n, h), self._kept = self._kept, None
         hidden, f32 = self.gate.shape[0], torch.float32
         down = F.qgtc_fp8_product(F.qgtc_fp8_quantize(dy, columns=True), F.qgtc_fp8_quantize(h, columns=True), f32)

@@ -234,3 +234,35 @@ def test_recorded_on_the_device_of_its_inputs(monkeypatch):
     assert streams[0] is not None and streams[0].device.index == index == y.get_device()
     torch.cuda.synchronize(index)
     assert torch.equal(y, b.forward(x)[0])
+
+
+def test_gradients_are_of_the_weights_packed_last():
+    """Weights that were packed while the block was not training."""
+    b = block(256, 300, torch.bfloat16, "silu", training=True)
+    x, dy = (U.activations(20, 256, k).bfloat16().cuda() for k in (1, 2))
+    b.forward(x)
+    b.backward(dy)
+    b.training = False
+    b.gate, b.up = (U.weights(300, 256, k).bfloat16().cuda() for k in (20, 21))
+    b.down = U.weights(256, 300, 22).bfloat16().cuda()
+    b.pack()
+    b.training = True
+    fresh = GatedFeedForward(b.norm_weight, b.gate, b.up, b.down, training=True)
+    assert torch.equal(b.forward(x)[0], fresh.forward(x)[0])
+    got, want = b.backward(dy), fresh.backward(dy)
+    assert set(got) == set(want) and all(torch.equal(got[k], want[k]) for k in got)
+
+
+def test_training_set_later():
+    """A block made without: backward() wants its weights packed for it, and then it is as one made with."""
+    b, want = (block(256, 300, torch.bfloat16, "gelu", training=t) for t in (False, True))
+    x, dy = (U.activations(20, 256, k).bfloat16().cuda() for k in (1, 2))
+    b.training = True
+    b.forward(x)
+    with pytest.raises(RuntimeError, match="pack"):
+        b.backward(dy)
+    b.pack()
+    b.forward(x)
+    want.forward(x)
+    got, want = b.backward(dy), want.backward(dy)
+    assert all(torch.equal(got[k], want[k]) for k in want)
