@@ -36,7 +36,9 @@ class GatedFeedForward:
         """Weights into 8-bit floats; to be called again when any of them has changed, or when training has been set on a block that
         was made without.  For training also along the other axis, as the backward pass contracts over it: once a block has those,
         every call brings them up to date, whether it is training then or not.  Weights of the sizes and the device of before go
-        where those were, since a recorded pass reads them there: passes on other streams have to be done with them."""
+        where those were, since a recorded pass reads them there: passes on other streams have to be done with them.  What a forward
+        pass has kept for backward() is of the weights before, and is let go."""
+        self._kept = None
         self.gate_q, self.up_q = _packed(self.gate, self.gate_q), _packed(self.up, self.up_q)
         self.down_q = _packed(self.down, self.down_q)
         if self.training or self.down_t is not None:
@@ -48,13 +50,13 @@ class GatedFeedForward:
         n = F.qgtc_rms_norm(x, self.norm_weight, self.eps, residual=residual, y=self.training, rstd=self.training)
         h = torch.empty((x.shape[0], self.gate.shape[0]), dtype=x.dtype, device=x.device) if self.training else None
         hq = F.qgtc_fp8_gated(n.fp8, self.gate_q, self.up_q, self.act, h=h)
-        if self.training:
-            self._kept = (n, h)
+        self._kept = (n, h) if self.training else None
         return F.qgtc_fp8_product(hq, self.down_q, x.dtype), n.sum
 
     def backward(self, dy: torch.Tensor, dsum: torch.Tensor | None = None) -> dict:
         """Gradients of the last forward() from that of y and, unless None, that of s: of x and of the residual ("x", one for both)
-        and of the weights ("norm_weight", "gate", "up", "down": float32).  Quantization counts as the identity."""
+        and of the weights ("norm_weight", "gate", "up", "down": float32).  Quantization counts as the identity.  Until then x (where
+        there was no residual) and norm_weight hold what they did: they are read again."""
         if self._kept is None:
             raise RuntimeError("backward() follows a forward() of a block that is training")
         if self.down_t is None:

@@ -266,3 +266,20 @@ def test_training_set_later():
     want.forward(x)
     got, want = b.backward(dy), want.backward(dy)
     assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+def test_packing_lets_go_of_a_forward_pass():
+    """Between a forward pass and its gradients weights are not exchanged, and there is no other forward pass."""
+    b = block(256, 300, torch.bfloat16, "silu", training=True)
+    x, dy = (U.activations(20, 256, k).bfloat16().cuda() for k in (1, 2))
+    b.forward(x)
+    b.gate.copy_(U.weights(300, 256, 20))
+    b.pack()
+    with pytest.raises(RuntimeError, match="forward"):
+        b.backward(dy)
+    b.forward(x)
+    b.training = False
+    b.forward(2 * x)
+    b.training = True
+    with pytest.raises(RuntimeError, match="forward"):
+        b.backward(dy)
