@@ -11,16 +11,21 @@ import torch
 from . import fp8 as F
 
 
+def _plain(w: torch.Tensor) -> torch.Tensor:
+    return w.detach() if w.requires_grad else w
+
+
 def _packed(w: torch.Tensor, old: F.Fp8 | None, columns: bool = False) -> F.Fp8:
     rows, cols = reversed(w.shape) if columns else w.shape
     if old is not None and (old.rows, old.cols, old.device) != (rows, cols, w.get_device()):
         old = None
-    return F.qgtc_fp8_quantize(w, columns=columns, out=old)
+    return F.qgtc_fp8_quantize(_plain(w), columns=columns, out=old)
 
 
 class GatedFeedForward:
     """norm_weight [D], gate and up [H, D], down [D, H]: float32, float16 or bfloat16 on one device, quantized once by pack().
-    training: forward() keeps its intermediate results until backward()."""
+    training: forward() keeps its intermediate results until backward(), which returns the gradients: parameters may be given, and
+    keep theirs to the caller."""
 
     def __init__(self, norm_weight: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor, eps: float = 1e-6,
                  act: str = "silu", training: bool = False):
@@ -43,11 +48,11 @@ class GatedFeedForward:
         self.down_q = _packed(self.down, self.down_q)
         if self.training or self.down_t is not None:
             self.down_t = _packed(self.down, self.down_t, columns=True)
-            self.gate_up_t = _packed(torch.cat([self.gate, self.up]), self.gate_up_t, columns=True)
+            self.gate_up_t = _packed(torch.cat([_plain(self.gate), _plain(self.up)]), self.gate_up_t, columns=True)
 
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
         """(y, s) of x [T, D]: the block's result, which the next norm adds to s."""
-        n = F.qgtc_rms_norm(x, self.norm_weight, self.eps, residual=residual, y=self.training, rstd=self.training)
+        n = F.qgtc_rms_norm(x, _plain(self.norm_weight), self.eps, residual=residual, y=self.training, rstd=self.training)
         h = torch.empty((x.shape[0], self.gate.shape[0]), dtype=x.dtype, device=x.device) if self.training else None
         hq = F.qgtc_fp8_gated(n.fp8, self.gate_q, self.up_q, self.act, h=h)
         self._kept = (n, h) if self.training else None
@@ -68,7 +73,7 @@ class GatedFeedForward:
         d = F.qgtc_fp8_gated_backward(n.fp8, self.gate_q, self.up_q, dh, self.act)
         gate_up = F.qgtc_fp8_product(F.qgtc_fp8_quantize(d, columns=True), F.qgtc_fp8_quantize(n.y, columns=True), f32)
         dn = F.qgtc_fp8_product(F.qgtc_fp8_quantize(d), self.gate_up_t, dy.dtype)
-        dx, dw = F.qgtc_rms_norm_backward(dn, n.sum, self.norm_weight, n.rstd, dsum=dsum)
+        dx, dw = F.qgtc_rms_norm_backward(dn, n.sum, _plain(self.norm_weight), n.rstd, dsum=dsum)
         return {"x": dx, "norm_weight": dw, "gate": gate_up[:hidden], "up": gate_up[hidden:], "down": down}
 
     def capture(self, x: torch.Tensor, residual: torch.Tensor | None = None):

@@ -1,6 +1,7 @@
 """8-bit floats: matrices of e4m3 codes with an e8m0 scale for every 128 entries of a row, and the operators
 on them (see include/qgtc.h).  As in binding.py the functions carry the names of the C entry points and only marshal:
-device memory is torch's, work goes to the current stream of the tensors' device."""
+device memory is torch's, work goes to the current stream of the tensors' device.  Nothing is recorded for autograd, gradients are
+calls of their own: a tensor that requires one is refused where torch would record (detach() it, or call under torch.no_grad())."""
 from __future__ import annotations
 
 import ctypes as C
@@ -53,6 +54,10 @@ def _bytes(fn, device: int, *args) -> int:
         return fn(*args)
 
 
+def _lost(what: str):
+    raise ValueError(f"{what}: requires a gradient, which this call does not record (detach it, or call under torch.no_grad())")
+
+
 def _matrix(t: torch.Tensor, what: str, device: int | None = None, shape=None, dtype=None) -> int:
     """Checks a row-major device matrix; its leading dimension."""
     size, step = t.shape, t.stride()
@@ -60,6 +65,8 @@ def _matrix(t: torch.Tensor, what: str, device: int | None = None, shape=None, d
         raise TypeError(f"{what}: a matrix of float32, float16 or bfloat16 is wanted, not {len(size)}-D {t.dtype}")
     if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{what}: {dtype} is wanted, not {t.dtype}")
+    if t.requires_grad and torch.is_grad_enabled():
+        _lost(what)
     if not t.is_cuda or (device is not None and t.get_device() != device):
         raise ValueError(f"{what}: not on the device of the other operands")
     if shape is not None and size != shape:
@@ -150,6 +157,8 @@ def qgtc_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, resi
     device, shape, dtype = x.get_device(), x.shape, x.dtype
     if weight.dtype not in _TYPES or weight.shape != (cols,) or not weight.is_contiguous() or weight.get_device() != device:
         raise ValueError("weight: one entry per column, contiguous, on x's device")
+    if weight.requires_grad and torch.is_grad_enabled():
+        _lost("weight")
     total, made, root = x, None, None
     p_res = p_sum = p_y = p_root = p_out = None
     ld_res = ld_sum = 0
@@ -188,6 +197,8 @@ def qgtc_rms_norm_backward(dy: torch.Tensor, sum: torch.Tensor, weight: torch.Te
     ld_dy = _matrix(dy, "dy", device, shape, dtype)
     if weight.dtype not in _TYPES or weight.shape != (cols,) or not weight.is_contiguous() or weight.get_device() != device:
         raise ValueError("weight: one entry per column, contiguous, on the sum's device")
+    if (weight.requires_grad or rstd.requires_grad) and torch.is_grad_enabled():
+        _lost("weight and rstd")
     if rstd.dtype != torch.float32 or rstd.shape != (rows,) or not rstd.is_contiguous() or rstd.get_device() != device:
         raise ValueError("rstd: one float32 entry per row, contiguous, on the sum's device")
     dx = out if out is not None else _strided(shape, (cols, 1), dtype=dtype, device=sum.device)

@@ -206,3 +206,16 @@ def test_plain_gate_slopes_are_differences(name):
     assert np.abs((U.act(name, g + step)[0] - U.act(name, g - step)[0]) / (2 * step) - s).max() < 1e-9
     assert np.abs((U.act(name, g + step)[1] - U.act(name, g - step)[1]) / (2 * step)).max() <= curve
     assert np.abs(s).max() <= 1.13
+
+
+@needs_lib
+def test_python_refuses_to_lose_gradients():
+    """Where torch would record: every operand that requires a gradient.  (Refused before a tensor's device is looked at.)"""
+    import paper_2111_09547_amd as q
+    x, g = torch.zeros((4, 256)), torch.zeros((4, 256), requires_grad=True)
+    for call in (lambda: q.qgtc_fp8_quantize(g), lambda: q.qgtc_fp8_quantize(g, columns=True), lambda: q.qgtc_rms_norm(g, torch.ones(256)),
+                 lambda: q.qgtc_rms_norm_backward(x, g, torch.ones(256), torch.ones(4))):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="device"):
+            call()

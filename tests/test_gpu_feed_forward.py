@@ -283,3 +283,28 @@ def test_packing_lets_go_of_a_forward_pass():
     b.training = True
     with pytest.raises(RuntimeError, match="forward"):
         b.backward(dy)
+
+
+def test_gradients_are_not_lost_silently():
+    """The operators refuse a tensor that requires a gradient; a block takes parameters, whose gradients backward() returns."""
+    b = block(256, 300, torch.float32, "silu", training=True)
+    x, dy = (U.activations(20, 256, k).cuda() for k in (1, 2))
+    xg, w, wg = x.clone().requires_grad_(), b.norm_weight, b.norm_weight.clone().requires_grad_()
+    n = q.qgtc_rms_norm(x, w, rstd=True)
+    h, hg = torch.empty((20, 300), device="cuda"), torch.empty((20, 300), device="cuda", requires_grad=True)
+    for call in (lambda: q.qgtc_rms_norm(xg, w), lambda: q.qgtc_rms_norm(x, wg), lambda: q.qgtc_rms_norm(x, w, residual=xg),
+                 lambda: q.qgtc_rms_norm_backward(xg, x, w, n.rstd), lambda: q.qgtc_rms_norm_backward(dy, x, wg, n.rstd),
+                 lambda: q.qgtc_rms_norm_backward(dy, x, w, n.rstd, dsum=xg), lambda: q.qgtc_fp8_product(n.fp8, b.gate_q, out=hg),
+                 lambda: q.qgtc_fp8_gated(n.fp8, b.gate_q, b.up_q, h=hg), lambda: q.qgtc_fp8_gated_backward(n.fp8, b.gate_q, b.up_q, hg),
+                 lambda: b.forward(xg), lambda: b.forward(x, xg)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    y, _ = b.forward(x)
+    want = b.backward(dy)
+    p = [torch.nn.Parameter(t) for t in (b.norm_weight, b.gate, b.up, b.down)]
+    c = GatedFeedForward(*p, training=True)
+    assert torch.equal(c.forward(x)[0], y)
+    got = c.backward(dy)
+    assert all(torch.equal(got[k], want[k]) for k in want)
