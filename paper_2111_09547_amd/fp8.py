@@ -103,8 +103,9 @@ class Fp8:
         if (step[1] != 1 and width > 1) or (apart[1] != 1 and wide[1] > 1):
             raise ValueError("rows have to be contiguous")
         self.codes, self.scales, self.device, self.rows, self.cols, self.blocks = codes, scales, device, rows, cols, blocks
-        self.c = B._Fp8C(codes.data_ptr(), scales.data_ptr(), rows, cols, step[0] if rows > 1 and width else width,
-                         apart[0] if rows > 1 and wide[1] else wide[1])
+        # (one row has no row to lie apart from: its tensor may have any width)
+        self.c = B._Fp8C(codes.data_ptr(), scales.data_ptr(), rows, cols, step[0] if rows > 1 and width else blocks * BLOCK,
+                         apart[0] if rows > 1 and wide[1] else blocks + 3 & ~3)
 
 
 def alloc_fp8(rows: int, cols: int, device) -> Fp8:

@@ -171,3 +171,16 @@ def test_product_of_blocks_without_a_scale(rows, cols, code):
             y = q.qgtc_fp8_product(*ops, dtype)
             y = y if side == 0 else y.t()
             assert bool(y[2].isnan().all()) and bool((y[:2] == 400).all()) and bool((y[3:] == 400).all())
+
+
+@pytest.mark.parametrize("width,words", [(256, 4), (300, 4), (1000, 7), (513, 6)])
+def test_one_row_of_any_width(width, words):
+    """A matrix of one row in tensors that are wider than its blocks, by any number of bytes."""
+    x = U.activations(1, 200, 1)
+    codes, scales = U.quantized(x.numpy())
+    c, s = torch.full((1, width), 99, dtype=torch.uint8, device="cuda"), torch.full((1, words), 98, dtype=torch.uint8, device="cuda")
+    m = q.qgtc_fp8_quantize(x.cuda(), out=q.Fp8(c, s, 200))
+    assert (U.raw(c)[:, :256] == codes).all() and (U.raw(s)[:, :2] == scales).all()
+    assert (U.raw(c)[:, 256:] == 99).all() and (U.raw(s)[:, 2:] == 98).all()
+    W = q.qgtc_fp8_quantize(U.weights(40, 200, 2).cuda())
+    assert torch.equal(q.qgtc_fp8_product(m, W), q.qgtc_fp8_product(q.qgtc_fp8_quantize(x.cuda()), W))
