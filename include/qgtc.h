@@ -738,7 +738,7 @@ qgtc_status qgtc_fp8_quantize(const void* src, int32_t type, int32_t rows, int32
  *   s    = x + residual, rounded to `type` (x itself without a residual)
  *   rstd = 1 / sqrt(mean of s^2 over the row + eps)
  *   y    = s * rstd * weight
- * in fp32, of s as it is rounded.  Any of the outputs may be left out (NULL):
+ * in fp32, of s as it is rounded.  Without rows or without columns nothing is written.  Any of the outputs may be left out (NULL):
  *   sum   s, in `type`; may be x or residual themselves (same leading dimension)
  *   rstd  [rows], for qgtc_rms_norm_backward
  *   y     in `type`

@@ -180,6 +180,8 @@ def qgtc_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, resi
         made = _strided(shape, (cols, 1), dtype=dtype, device=x.device)
         p_y = made.data_ptr()
     if rstd:
+        if not cols:
+            raise ValueError("rstd: x has no columns to take a mean of")
         root = _empty(rows, dtype=torch.float32, device=x.device)
         p_root = root.data_ptr()
     n = B._NormC(_TYPES[dtype], _TYPES[weight.dtype], rows, cols, eps, 0, x.data_ptr(), ld, p_res, ld_res, weight.data_ptr(),

@@ -184,3 +184,12 @@ def test_one_row_of_any_width(width, words):
     assert (U.raw(c)[:, 256:] == 99).all() and (U.raw(s)[:, 2:] == 98).all()
     W = q.qgtc_fp8_quantize(U.weights(40, 200, 2).cuda())
     assert torch.equal(q.qgtc_fp8_product(m, W), q.qgtc_fp8_product(q.qgtc_fp8_quantize(x.cuda()), W))
+
+
+def test_norm_without_columns():
+    """There is nothing in any output, and no mean for rstd to be made from."""
+    x, w = torch.empty((5, 0), device="cuda"), torch.empty(0, device="cuda")
+    n = q.qgtc_rms_norm(x, w, residual=x, y=True)
+    assert n.sum.shape == n.y.shape == (5, 0) and (n.fp8.rows, n.fp8.cols) == (5, 0)
+    with pytest.raises(ValueError, match="columns"):
+        q.qgtc_rms_norm(x, w, rstd=True)
