@@ -12,6 +12,7 @@ import torch
 from . import binding as B
 
 BLOCK = 128
+_MOST = 1 << 29                                          # rows and columns (sizes go to the library in 32 bits)
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _ACTS = {"silu": 0, "gelu": 1}
 
@@ -58,7 +59,7 @@ def _lost(what: str):
     raise ValueError(f"{what}: requires a gradient, which this call does not record (detach it, or call under torch.no_grad())")
 
 
-def _matrix(t: torch.Tensor, what: str, device: int | None = None, shape=None, dtype=None) -> int:
+def _matrix(t: torch.Tensor, what: str, device: int | None = None, shape=None, dtype=None, most: int = _MOST) -> int:
     """Checks a row-major device matrix; its leading dimension."""
     size, step = t.shape, t.stride()
     if len(size) != 2 or t.dtype not in _TYPES:
@@ -69,6 +70,8 @@ def _matrix(t: torch.Tensor, what: str, device: int | None = None, shape=None, d
         _lost(what)
     if not t.is_cuda or (device is not None and t.get_device() != device):
         raise ValueError(f"{what}: not on the device of the other operands")
+    if size[0] > _MOST or size[1] > most:
+        raise ValueError(f"{what}: at most 2^29 rows and columns, not {size[0]} x {size[1]}")
     if shape is not None and size != shape:
         raise ValueError(f"{what}: {shape[0]} x {shape[1]} is wanted, not {size[0]} x {size[1]}")
     if size[0] > 1:
@@ -96,6 +99,8 @@ class Fp8:
             raise ValueError("codes and scales: a row of each for a row of the matrix, on one device")
         if cols is None:
             cols = width
+        if rows > _MOST or cols > _MOST:
+            raise ValueError(f"at most 2^29 rows and columns, not {rows} x {cols}")
         blocks = (cols + 127) >> 7
         if cols < 0 or width < blocks * BLOCK or wide[1] < (blocks + 3 & ~3):
             raise ValueError("codes have room for whole blocks of 128, scales for a multiple of four")
@@ -110,6 +115,8 @@ class Fp8:
 
 def alloc_fp8(rows: int, cols: int, device) -> Fp8:
     """Room for a matrix; nothing of it is written yet."""
+    if rows > _MOST or cols > _MOST:
+        raise ValueError(f"at most 2^29 rows and columns, not {rows} x {cols}")
     m = Fp8.__new__(Fp8)
     m.rows, m.cols = rows, cols
     m.blocks = blocks = (cols + 127) >> 7
@@ -267,7 +274,7 @@ def qgtc_fp8_gated_backward(x: Fp8, gate: Fp8, up: Fp8, dh: torch.Tensor, act: s
     ld_dh = _matrix(dh, "dh", device, (rows, cols))
     if out is None:
         out = _empty((rows, 2 * cols), dtype=dh.dtype, device=dh.device)
-    ld = _matrix(out, "out", device, (rows, 2 * cols), dh.dtype)
+    ld = _matrix(out, "out", device, (rows, 2 * cols), dh.dtype, 2 * _MOST)
     to = out.data_ptr()
     _run(_L.qgtc_fp8_gated_backward, device, _byref(x.c), _byref(gate.c), _byref(up.c), _ACTS[act], _TYPES[dh.dtype],
          dh.data_ptr(), ld_dh, to, ld, to + cols * dh.element_size(), ld)

@@ -193,3 +193,15 @@ def test_norm_without_columns():
     assert n.sum.shape == n.y.shape == (5, 0) and (n.fp8.rows, n.fp8.cols) == (5, 0)
     with pytest.raises(ValueError, match="columns"):
         q.qgtc_rms_norm(x, w, rstd=True)
+
+
+def test_sizes_beyond_32_bits():
+    """2^32 and some rows or columns are refused, and not taken for the few that 32 bits make of them."""
+    n = (1 << 32) + 5
+    tall = torch.empty((n, 1), dtype=torch.bfloat16, device="cuda")                # 8 GB
+    one = torch.ones(1, device="cuda")
+    for call in (lambda: q.qgtc_rms_norm(tall, one, fp8=False, y=True), lambda: q.qgtc_fp8_quantize(tall, columns=True),
+                 lambda: q.qgtc_fp8_quantize(tall.t()), lambda: q.alloc_fp8(1, n, "cuda"),
+                 lambda: q.Fp8(tall.view(torch.uint8).view(1, 2 * n), torch.empty((1, 4), dtype=torch.uint8, device="cuda"), n)):
+        with pytest.raises(ValueError, match="2\\^29"):
+            call()
