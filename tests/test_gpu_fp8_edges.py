@@ -205,3 +205,62 @@ def test_sizes_beyond_32_bits():
                  lambda: q.Fp8(tall.view(torch.uint8).view(1, 2 * n), torch.empty((1, 4), dtype=torch.uint8, device="cuda"), n)):
         with pytest.raises(ValueError, match="2\\^29"):
             call()
+
+
+# ---- more than one launch takes: what is written at the border between two launches and at the end ------------------------------------
+def test_quantize_rows_in_two_launches():
+    """2^25 waves of four rows a launch."""
+    first, rows = 1 << 27, (1 << 27) + 70
+    x = torch.ones((rows, 1), dtype=torch.bfloat16, device="cuda")
+    for i, r in enumerate((0, first - 1, first, first + 1, rows - 1)):
+        x[r] = 3.0 * 2.0 ** i
+    m = q.qgtc_fp8_quantize(x)                               # 17 GB of codes
+    for part in (slice(0, 40), slice(first - 40, first + 40), slice(rows - 40, rows)):
+        assert torch.equal(m.codes[part, :1].float() * m.scales[part, :1].float(), x[part].float())
+        assert bool((m.codes[part, 1:].view(torch.uint8) == 0).all())
+
+
+def test_quantize_columns_in_two_launches():
+    """65535 blocks of rows a launch."""
+    first, rows = 65535 * 128, 65535 * 128 + 333
+    x = torch.randn((rows, 3), device="cuda", generator=torch.Generator("cuda").manual_seed(1)).bfloat16()
+    m, a, b = (q.qgtc_fp8_quantize(t, columns=True) for t in (x, x[:first], x[first:]))
+    for name, cut in (("codes", first), ("scales", first // 128)):
+        whole, head, tail = (getattr(t, name).view(torch.uint8) for t in (m, a, b))
+        n = b.blocks * 128 if name == "codes" else b.blocks
+        assert torch.equal(whole[:, :cut], head[:, :cut]) and torch.equal(whole[:, cut:cut + n], tail[:, :n])
+
+
+def counted(rows, at):
+    """rows x 128 in 8-bit floats with scale 1: 64 at column 0, and 1 + row % 13 at column `at`."""
+    codes = torch.zeros((rows, 128), dtype=torch.uint8, device="cuda")
+    n = (1 + torch.arange(rows, device="cuda") % 13).float()
+    codes[:, 0] = 0x68                                       # 2^6
+    codes[:, at] = n.to(torch.float8_e4m3fn).view(torch.uint8)
+    return q.Fp8(codes, torch.full((rows, 4), 127, dtype=torch.uint8, device="cuda"), 128), n
+
+
+def test_product_of_few_in_two_launches_of_rows():
+    """65535 times 64 rows of X a launch, results in fp32."""
+    (X, n), (W, k) = counted(65535 * 64 + 70, 1), counted(5, 1)
+    assert torch.equal(q.qgtc_fp8_product(X, W, torch.float32), 4096 + n[:, None] * k[None, :])
+
+
+def test_product_of_few_in_two_launches_of_columns():
+    """2^26 rows of W a launch, results in fp32."""
+    (X, n), (W, k) = counted(3, 1), counted((1 << 26) + 40, 1)
+    y = q.qgtc_fp8_product(X, W, torch.float32)
+    for i in range(3):
+        assert torch.equal(y[i], 4096 + n[i] * k)
+
+
+def test_gated_rows_in_two_launches():
+    """2^25 waves, each with up to 512 columns of a row, a launch of what makes 8-bit floats of the gated results."""
+    rows = (1 << 25) + 70
+    X, n = counted(rows, 1)
+    one = torch.zeros((2, 1, 128), device="cuda")
+    one[0, 0, 0], one[1, 0, 1] = 1.0, 1.0
+    m = q.qgtc_fp8_gated(X, *(q.qgtc_fp8_quantize(t) for t in one))          # silu(64) = 64, times n
+    assert torch.equal(m.codes[:, 0].float() * m.scales[:, 0].float(), 64 * n)
+    for part in (slice(0, 40), slice((1 << 25) - 40, (1 << 25) + 40), slice(rows - 40, rows)):
+        assert bool((m.codes[part, 1:].view(torch.uint8) == 0).all())
