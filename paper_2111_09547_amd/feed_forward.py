@@ -66,7 +66,7 @@ class GatedFeedForward:
             raise RuntimeError("backward() follows a forward() of a block that is training")
         if self.down_t is None:
             raise RuntimeError("the block was packed for forward passes alone: pack() once more")
-        (n, h), self._kept = self._kept, None
+        n, h = self._kept
         hidden, f32 = self.gate.shape[0], torch.float32
         down = F.qgtc_fp8_product(F.qgtc_fp8_quantize(dy, columns=True), F.qgtc_fp8_quantize(h, columns=True), f32)
         dh = F.qgtc_fp8_product(F.qgtc_fp8_quantize(dy), self.down_t, dy.dtype)
@@ -74,6 +74,7 @@ class GatedFeedForward:
         gate_up = F.qgtc_fp8_product(F.qgtc_fp8_quantize(d, columns=True), F.qgtc_fp8_quantize(n.y, columns=True), f32)
         dn = F.qgtc_fp8_product(F.qgtc_fp8_quantize(d), self.gate_up_t, dy.dtype)
         dx, dw = F.qgtc_rms_norm_backward(dn, n.sum, _plain(self.norm_weight), n.rstd, dsum=dsum)
+        self._kept = None                                # (a gradient that was refused can be given again)
         return {"x": dx, "norm_weight": dw, "gate": gate_up[:hidden], "up": gate_up[hidden:], "down": down}
 
     def capture(self, x: torch.Tensor, residual: torch.Tensor | None = None):

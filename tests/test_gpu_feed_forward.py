@@ -308,3 +308,18 @@ def test_gradients_are_not_lost_silently():
     assert torch.equal(c.forward(x)[0], y)
     got = c.backward(dy)
     assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+def test_a_refused_gradient_can_be_given_again():
+    b = block(256, 300, torch.bfloat16, "silu", training=True)
+    x, dy = (U.activations(20, 256, k).bfloat16().cuda() for k in (1, 2))
+    b.forward(x)
+    want = b.backward(dy)
+    b.forward(x)
+    for bad, error in ((dy.float(), TypeError), (dy[:19], q.QgtcError), (dy[:, :128], q.QgtcError)):
+        with pytest.raises(error):
+            b.backward(bad)
+    with pytest.raises(ValueError):
+        b.backward(dy, dy[:19])
+    got = b.backward(dy)
+    assert all(torch.equal(got[k], want[k]) for k in want)
