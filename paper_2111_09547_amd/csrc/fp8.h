@@ -11,7 +11,7 @@ constexpr int kMostEntries = 1 << 29;              // rows, and columns, of one 
 constexpr int64_t kMostThreads = (int64_t)1 << 31; // of a launch along an axis (their number has 32 bits): what is more takes several
 
 inline int fp8_blocks(int cols) { return cdiv(cols, kBlock); }
-qgtc_status check_fp8(const qgtc_fp8* m);          // fp8.hip
+qgtc_status check_fp8(const qgtc_fp8* m);          // quantize.hip
 inline bool float_type(int type) { return type == QGTC_F32 || type == QGTC_F16 || type == QGTC_BF16; }
 inline int float_bytes(int type) { return type == QGTC_F32 ? 4 : 2; }
 // A row-major tensor of rows x cols with leading dimension ld.

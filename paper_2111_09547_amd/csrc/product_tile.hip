@@ -10,16 +10,16 @@
 // the quarters in front have left.  There is a barrier in the middle of a step and at its end, behind which the halves that
 // have just been read are loaded for the step after the next: each has one and a half steps to come (with one barrier, and so
 // one step, waves waited a third of the time).  Nothing in the loop may use vector memory in the compiler's own way: its waits are
-// for everything that is on its way (one word of scratch in the loop: 8192 cubed 520 us, without it 435).
+// for everything that is on its way (one word of scratch in the loop: a fifth more time for 8192 cubed).
 //
 // Workgroups stay and take several tiles: the loads run on to the next tile while one is finished (a workgroup per tile lost
-// 19 us a tile with that: 4096 x 16384 x 4096 256 us).
+// 19 us a tile with that, 7 % of 4096 x 16384 x 4096).
 //
 // A row of a buffer is 128 bytes; its 16-byte piece c lies at c ^ (row % 8), so that 16 lanes reading a piece each of 16 rows meet
 // every bank once.  W's rows are put into the buffer in another order: register i of lane group g of the t-th 16 of 64 belongs
 // to row 32 (t / 2) + 8 g + 4 (t % 2) + i of them, so that a lane ends up with twice eight results that lie side by side, and four
 // lanes with 32, or, where results are bytes, to row 16 g + 4 t + i, and a lane has 16 side by side: 64 bytes of a row for a store
-// either way (the other order for bytes: gated 4096 x 4096 x 8192 233 instead of 226 us).
+// either way (the other order for bytes: 3 % more for gated 4096 x 4096 x 8192).
 #include "product_lds.h"
 
 namespace qgtc {
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(256, 1) void tile_kernel(const TileParams tp) {
   typedef typename Float<TYPE>::type T;
   auto finish = [&](uint32_t tile) {
     // (Anew for every tile: what the compiler makes of these once for all tiles it keeps in scratch memory, and each load of it from
-    // there waits for everything that is on its way: gated 4096 x 4096 x 8192 253 us, so 233.)
+    // there waits for everything that is on its way: 8 % of gated 4096 x 4096 x 8192.)
     int own = lane;
     asm volatile("" : "+v"(own));
     const int r = own & 15, g = own >> 4;
