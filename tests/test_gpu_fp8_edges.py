@@ -264,3 +264,43 @@ def test_gated_rows_in_two_launches():
     assert torch.equal(m.codes[:, 0].float() * m.scales[:, 0].float(), 64 * n)
     for part in (slice(0, 40), slice((1 << 25) - 40, (1 << 25) + 40), slice(rows - 40, rows)):
         assert bool((m.codes[part, 1:].view(torch.uint8) == 0).all())
+
+
+# ---- operands and results in wider memory: the same bits -----------------------------------------------------------------------------
+def apart(m, codes_by, scales_by):
+    """m in memory whose rows lie further apart, with other bytes between them."""
+    c = torch.full((m.rows, m.blocks * 128 + 128 * codes_by), 0x7f, dtype=torch.uint8, device="cuda")
+    s = torch.full((m.rows, m.scales.shape[1] + 4 * scales_by), 255, dtype=torch.uint8, device="cuda")
+    c[:, :m.blocks * 128] = m.codes.view(torch.uint8)[:, :m.blocks * 128]
+    s[:, :m.blocks] = m.scales.view(torch.uint8)[:, :m.blocks]
+    return q.Fp8(c, s, m.cols)
+
+
+def within(t, left, right):
+    buf = torch.full((t.shape[0], t.shape[1] + left + right), 7.0, dtype=t.dtype, device="cuda")
+    v = buf[:, left:left + t.shape[1]]
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("rows,cols,inner", SIZES + [(40, 300, 1100), (700, 1030, 260), (4090, 4090, 200)])
+def test_gated_of_matrices_within_others(rows, cols, inner):
+    """X, G, U, h, the gradient and the results each with a pitch of its own."""
+    X, G, P = (q.qgtc_fp8_quantize(t.cuda()) for t in (U.activations(rows, inner, 1), U.weights(cols, inner, 2), U.weights(cols, inner, 3)))
+    x, g, p = apart(X, 1, 3), apart(G, 2, 1), apart(P, 5, 2)
+    for dtype in (torch.bfloat16, torch.float16, torch.float32):
+        h, h2 = (torch.zeros((rows, cols), dtype=dtype, device="cuda") for _ in range(2))
+        h2 = within(h2, 3, 2)
+        want = q.qgtc_fp8_gated(X, G, P, h=h)
+        out = apart(want, 3, 2)
+        before = out.codes.clone(), out.scales.clone()
+        out.codes[:, :want.blocks * 128], out.scales[:, :want.blocks] = 99, 99
+        q.qgtc_fp8_gated(x, g, p, out=out, h=h2)
+        assert torch.equal(h2, h) and torch.equal(out.codes, before[0]) and torch.equal(out.scales, before[1])
+        dh = torch.randn((rows, cols), device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(dtype)
+        d = q.qgtc_fp8_gated_backward(X, G, P, dh, "gelu")
+        d2 = within(torch.zeros_like(d), 1, 4)
+        q.qgtc_fp8_gated_backward(x, g, p, within(dh, 5, 3), "gelu", out=d2)
+        assert torch.equal(d2, d)
+        y = q.qgtc_fp8_product(X, G, dtype)
+        assert torch.equal(q.qgtc_fp8_product(x, g, out=within(torch.zeros_like(y), 3, 4)), y)
