@@ -89,10 +89,11 @@ __global__ __launch_bounds__(512) void few_kernel(const ProductParams p) {
       int again = r;
       asm volatile("" : "+v"(again));                  // (addresses that are kept for this cost the loop above its registers)
       aim(again);
+      v4f other[D][MT];
 #pragma unroll
       for (int d = 0; d < D; ++d)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[d][t] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = 0; t < MT; ++t) other[d][t] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
       for (int b = wave * 4; b < p.blocks; b += (b & 3) == 3 ? waves * 4 - 3 : 1) {
         const int64_t at = (int64_t)b * kBlock;
@@ -111,9 +112,13 @@ __global__ __launch_bounds__(512) void few_kernel(const ProductParams p) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) rows[i] = __shfl((int)sw, 4 * g + i);
 #pragma unroll
-          for (int t = 0; t < MT; ++t) acc[d][t] = apart_mfma(w, x[t], acc[d][t], rows, 0, sx[t]);
+          for (int t = 0; t < MT; ++t) other[d][t] = apart_mfma(w, x[t], other[d][t], rows, 0, sx[t]);
         }
       }
+#pragma unroll
+      for (int d = 0; d < D; ++d)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) take_apart(acc[d][t], other[d][t]);
     }
   }
 #pragma unroll

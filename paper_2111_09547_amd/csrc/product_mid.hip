@@ -90,8 +90,7 @@ __global__ __launch_bounds__(256, 1) void mid_kernel(const MidParams mp) {
       (o ? b.sw : b.sx)[t] = lds[(o ? sw_at : sx_at) + s_at + (uint32_t)(t * 64)];
     }
   };
-  v4f acc[4][4];                                     // [w][x]
-  auto sums = [&](auto way) {
+  auto sums = [&](auto way, v4f (&acc)[4][4]) {      // [w][x]
     constexpr bool APART = decltype(way)::value;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -143,7 +142,8 @@ __global__ __launch_bounds__(256, 1) void mid_kernel(const MidParams mp) {
     if (p.blocks & 1) step(p.blocks - 1, b0, b1);
     meet<0>();                                       // (nothing is on its way to LDS any more)
   };
-  sums(std::false_type());
+  v4f acc[4][4];
+  sums(std::false_type(), acc);
   if constexpr (WIDE) {                              // (waves share their loads, so all of them again or none)
     bool none = false;
 #pragma unroll
@@ -154,7 +154,14 @@ __global__ __launch_bounds__(256, 1) void mid_kernel(const MidParams mp) {
     const uint32_t mine = __ballot(none) != 0ull;
     if (lane == 0) flags[wave] = mine;
     meet_lds();
-    if (scalar(flags[0] | flags[1] | flags[2] | flags[3])) sums(std::true_type());
+    if (scalar(flags[0] | flags[1] | flags[2] | flags[3])) {
+      v4f other[4][4];
+      sums(std::true_type(), other);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) take_apart(acc[t][u], other[t][u]);
+    }
   }
 
   // ---- what is made of the sums ----

@@ -304,3 +304,17 @@ def test_gated_of_matrices_within_others(rows, cols, inner):
         assert torch.equal(d2, d)
         y = q.qgtc_fp8_product(X, G, dtype)
         assert torch.equal(q.qgtc_fp8_product(x, g, out=within(torch.zeros_like(y), 3, 4)), y)
+
+
+@pytest.mark.parametrize("rows,cols", SCALED[:3])
+def test_rows_in_fp32_keep_to_themselves(rows, cols):
+    """A row that has a NaN, or numbers whose sums leave fp32's range on the way: no bit of the other rows' results changes."""
+    x, w = U.activations(rows, 900, 1), U.weights(cols, 900, 2)
+    W = q.qgtc_fp8_quantize(w.cuda())
+    want = q.qgtc_fp8_product(q.qgtc_fp8_quantize(x.cuda()), W, torch.float32)
+    for r, v in ((0, float("nan")), (rows - 1, 3e38), (rows // 2, float("inf"))):
+        bad = x.clone()
+        bad[r, 77] = v
+        got = q.qgtc_fp8_product(q.qgtc_fp8_quantize(bad.cuda()), W, torch.float32)
+        keep = torch.arange(rows) != r
+        assert torch.equal(got[keep], want[keep]) and not torch.equal(got[r], want[r])
