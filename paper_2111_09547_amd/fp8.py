@@ -59,7 +59,7 @@ def _lost(what: str):
     raise ValueError(f"{what}: requires a gradient, which this call does not record (detach it, or call under torch.no_grad())")
 
 
-def _matrix(t: torch.Tensor, what: str, device: int | None = None, shape=None, dtype=None, most: int = _MOST) -> int:
+def _matrix(t: torch.Tensor, what: str, device: int | None = None, shape=None, dtype=None) -> int:
     """Checks a row-major device matrix; its leading dimension."""
     size, step = t.shape, t.stride()
     if len(size) != 2 or t.dtype not in _TYPES:
@@ -70,9 +70,10 @@ def _matrix(t: torch.Tensor, what: str, device: int | None = None, shape=None, d
         _lost(what)
     if not t.is_cuda or (device is not None and t.get_device() != device):
         raise ValueError(f"{what}: not on the device of the other operands")
-    if size[0] > _MOST or size[1] > most:
-        raise ValueError(f"{what}: at most 2^29 rows and columns, not {size[0]} x {size[1]}")
-    if shape is not None and size != shape:
+    if shape is None:
+        if max(size) > _MOST:
+            raise ValueError(f"{what}: at most 2^29 rows and columns, not {size[0]} x {size[1]}")
+    elif size != shape:
         raise ValueError(f"{what}: {shape[0]} x {shape[1]} is wanted, not {size[0]} x {size[1]}")
     if size[0] > 1:
         if step[1] != 1 and size[1] > 1:
@@ -117,6 +118,10 @@ def alloc_fp8(rows: int, cols: int, device) -> Fp8:
     """Room for a matrix; nothing of it is written yet."""
     if rows > _MOST or cols > _MOST:
         raise ValueError(f"at most 2^29 rows and columns, not {rows} x {cols}")
+    return _room(rows, cols, device)
+
+
+def _room(rows: int, cols: int, device) -> Fp8:
     m = Fp8.__new__(Fp8)
     m.rows, m.cols = rows, cols
     m.blocks = blocks = (cols + 127) >> 7
@@ -132,7 +137,7 @@ def alloc_fp8(rows: int, cols: int, device) -> Fp8:
 
 def _result(out: Fp8 | None, rows: int, cols: int, like: torch.Tensor) -> Fp8:
     if out is None:
-        return alloc_fp8(rows, cols, like.device)
+        return _room(rows, cols, like.device)
     if out.rows != rows or out.cols != cols or out.device != like.get_device():
         raise ValueError(f"out: {rows} x {cols} on the operands' device is wanted, not {out.rows} x {out.cols}")
     return out
@@ -274,7 +279,7 @@ def qgtc_fp8_gated_backward(x: Fp8, gate: Fp8, up: Fp8, dh: torch.Tensor, act: s
     ld_dh = _matrix(dh, "dh", device, (rows, cols))
     if out is None:
         out = _empty((rows, 2 * cols), dtype=dh.dtype, device=dh.device)
-    ld = _matrix(out, "out", device, (rows, 2 * cols), dh.dtype, 2 * _MOST)
+    ld = _matrix(out, "out", device, (rows, 2 * cols), dh.dtype)
     to = out.data_ptr()
     _run(_L.qgtc_fp8_gated_backward, device, _byref(x.c), _byref(gate.c), _byref(up.c), _ACTS[act], _TYPES[dh.dtype],
          dh.data_ptr(), ld_dh, to, ld, to + cols * dh.element_size(), ld)
